@@ -53,7 +53,8 @@ typedef enum {
     LORY_ERR_ALIGN = 4,     /* a pointer is not 16-byte aligned */
     LORY_ERR_WORKSPACE = 5, /* workspace_bytes is smaller than lory_workspace_bytes() reports (than the
                                least a call takes, where its description names one) */
-    LORY_ERR_DEVICE = 6     /* a HIP call or kernel launch failed */
+    LORY_ERR_DEVICE = 6,    /* a HIP call or kernel launch failed */
+    LORY_ERR_OVERLAP = 7    /* an output overlaps another buffer of the call where that is not allowed */
 } lory_status;
 
 typedef enum { LORY_F32 = 0, LORY_BF16 = 1 } lory_dtype;
@@ -327,6 +328,157 @@ int lory_merged_ffn_bwd(const lory_shape *shape, const void *X, const float *w,
                         void *dX, void *dWg, void *dWu, void *dWd,
                         int grad_dtype, int accumulate, float *dw,
                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The attention half of the block around the layer: the plan of a generating
+ * step over a paged key-value cache, the norms of the query and key heads with
+ * the position rotation (alone, with the store into the cache, and its
+ * gradient), and the attention of one new token per row over the cache.
+ *
+ * Differences to the conventions above: counts that follow from the traffic
+ * (tokens, rows, room) may be 0, and with 0 of them the pointers that hold them
+ * may be NULL; integer and double arrays are aligned to their element only; heads are
+ * strided.  `lory_heads` is a [tokens, heads, head_dim] tensor whose last index
+ * is contiguous; token and head are its strides in elements, >= 0.  data is
+ * 16-byte aligned and both strides are multiples of 16 bytes (slices of one
+ * [tokens, (q_heads + 2 kv_heads) * head_dim] product are passed as they lie;
+ * the stride of a dimension of one entry is not used).  Inputs are read only.
+ * Outputs whose strides make heads share a place are LORY_ERR_OVERLAP.
+ * head_dim % 8 == 0, 8 <= head_dim <= 256; q_heads and kv_heads up to 65535;
+ * tokens <= 2^25.
+ */
+typedef struct {
+    void *data;
+    int64_t token, head;
+} lory_heads;
+
+typedef struct {
+    int32_t tokens, q_heads, kv_heads, head_dim;
+    int32_t rot_dim;     /* the first rot_dim values of a head turn; a multiple of 16, 0 <= rot_dim <= head_dim */
+    int32_t interleaved; /* pairs are (2i, 2i+1) if 1, (i, i + rot_dim/2) if 0 */
+    int32_t dtype;       /* lory_dtype of the heads, the norm weights and the cache */
+    float eps;           /* added to the mean square; >= 0 */
+} lory_rope_shape;
+
+/*
+ * Norm of every query and key head, then the position rotation of its first
+ * rot_dim values.  For a head x of the token at position p:
+ *   y = x / sqrt(mean(x^2) + eps) * w          (y = x where wq and wk are NULL)
+ *   (y_a, y_b) <- (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = p * freq[i]
+ * for pair i (a, b as `interleaved` says).
+ * in:  q [tokens, q_heads, head_dim], k [tokens, kv_heads, head_dim]; pos [tokens]
+ *      int32 (any sign); freq [rot_dim/2] fp64, radians per position; wq, wk
+ *      [head_dim] (dtype, 16-byte aligned), both or neither
+ * out: q_out, k_out, shaped like q and k.  An output may be its own input in
+ *      place (same data and strides); any other overlap is undefined.
+ * Angles are formed in fp64 and reduced to one turn there, so positions of any
+ * size keep fp32 accuracy; everything else is fp32, rounded once.
+ */
+int lory_qk_rope(const lory_rope_shape *shape, const lory_heads *q, const lory_heads *k,
+                 const int32_t *pos, const double *freq, const void *wq, const void *wk,
+                 const lory_heads *q_out, const lory_heads *k_out, void *stream);
+
+/*
+ * lory_qk_rope whose keys, with the values beside them, go into a paged cache
+ * instead of k_out:
+ *   cache [pages, kv_heads, page, head_dim], contiguous, keys and values each
+ * Token t goes to page slots[t] / page, row slots[t] % page; slots outside
+ * [0, pages * page) store nothing (-1 is what lory_kv_plan gives positions of
+ * its buffers that no token fills).  Two tokens with one slot: either may win.
+ * in:  v [tokens, kv_heads, head_dim]; slots [tokens] int64; the rest as above
+ * out: q_out; the slots' rows of k_cache and v_cache, nothing else of them.
+ */
+int lory_qk_rope_cache(const lory_rope_shape *shape, const lory_heads *q, const lory_heads *k, const lory_heads *v,
+                       const int32_t *pos, const double *freq, const void *wq, const void *wk,
+                       const lory_heads *q_out, void *k_cache, void *v_cache, int32_t pages, int32_t page,
+                       const int64_t *slots, void *stream);
+
+/*
+ * Gradient of lory_qk_rope.  With g = the gradient of y turned back by -t,
+ * r = 1/sqrt(mean(x^2) + eps) and n = r x:
+ *   dx = r (g w - n mean(g w n));   dw = sum over tokens and heads of g n
+ * in:  q, k as the forward had them (not read where wq and wk are NULL: then
+ *      dx = g); dq_out, dk_out, the gradients of its outputs; pos, freq, wq, wk, eps
+ * out: dq, dk (dtype; may be dq_out, dk_out in place); dwq, dwk [head_dim] fp32,
+ *      overwritten (0 for 0 tokens), not touched and may be NULL without weights.
+ * Sums run in a fixed order (bit-reproducible).
+ * workspace: lory_qk_rope_workspace_bytes(shape); its contents are undefined
+ * before and after a call.  Without weights 0 bytes and NULL are enough.
+ */
+int lory_qk_rope_workspace_bytes(const lory_rope_shape *shape, size_t *bytes_out);
+int lory_qk_rope_bwd(const lory_rope_shape *shape, const lory_heads *q, const lory_heads *k,
+                     const lory_heads *dq_out, const lory_heads *dk_out, const int32_t *pos, const double *freq,
+                     const void *wq, const void *wk, const lory_heads *dq, const lory_heads *dk, float *dwq, float *dwk,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Plan of one step: pages for the new tokens of every request, and where each
+ * token goes.  Row b has lens[b] cached tokens and adds add[b] (>= 0), or has
+ * ended (add[b] < 0) and gives its pages back.
+ *   pages of n tokens = ceil(n / page); table[b][c] is the page of tokens
+ *   [c * page, (c+1) * page) of row b
+ *   free is a stack of count[0] pages, its top at free[count[0] - 1].  Pages of
+ *   ended rows go on top first, rows in order and each row's pages in order; then
+ *   rows take theirs from the top, in order.
+ * in:     lens, add [rows]; count [1]
+ * in/out: table [rows, width] int32, table_row elements from row to row (entries of pages that rows take
+ *         are written; those of ended rows stay as they are); free [free_size] int32
+ * out:    lens_new [rows] (0 for ended rows); cu [rows + 1], the sum of the added
+ *         tokens before each row; positions [room] int32 and slots [room] int64 of
+ *         the new tokens, row after row (position 0 and slot -1 past the last);
+ *         count_new [1]; status [1]: 0, or the sum of
+ *           1  more than `room` new tokens         2  a row longer than width * page
+ *           4  not enough free pages               8  more than free_size free pages
+ *          16  a length below 0 or (of an ended row) above width * page, or a count
+ *              outside [0, free_size]
+ * With a status other than 0 nothing is planned: table and free stay, lens_new =
+ * lens, count_new = count, cu = 0, positions = 0, slots = -1.  The status
+ * stays on the device: nothing waits for it.
+ * All arrays are int32 except slots.  No output may overlap another array
+ * (LORY_ERR_OVERLAP): a program keeps two sets of lens and count and swaps them.
+ * Calling again with the same lens, add and count gives the same plan.
+ * 1 <= page, width, free_size; width * page < 2^31; rows <= 2^20.  Needs no workspace.
+ */
+typedef struct {
+    int32_t rows, width, page, free_size, room;
+    int64_t table_row;
+} lory_plan_shape;
+int lory_kv_plan(const lory_plan_shape *shape, const int32_t *lens, const int32_t *add, int32_t *table, int32_t *free,
+                 const int32_t *count, int32_t *lens_new, int32_t *cu, int32_t *positions, int64_t *slots,
+                 int32_t *count_new, int32_t *status, void *stream);
+
+/*
+ * Attention of one new token per row over its cached keys and values:
+ *   z[t] = scale * <q[b,h], K[b,t,h']>,  out[b,h] = sum_t softmax(z)[t] V[b,t,h'],
+ *   lse[b,h] = log sum_t exp(z[t]),      t < lens[b],  h' = h / (q_heads / kv_heads)
+ * with K[b,t,h'] = k_cache[table[b][t / page]][h'][t % page].
+ * in:  q [rows, q_heads, head_dim] (strided heads); k_cache, v_cache [pages,
+ *      kv_heads, page, head_dim] contiguous; table [rows, width] int32, table_row
+ *      elements from row to row; lens [rows] int32
+ * out: out [rows, q_heads, head_dim] (strided heads, may be q in place: same data
+ *      and strides); lse [rows, q_heads] fp32 or NULL
+ * Rows without a token (lens <= 0), and heads whose scores are all -inf, give 0
+ * and lse -inf.  Lengths above width * page count as that.  A token whose page is
+ * outside [0, pages) is left out.  What the cache holds behind a row's last token
+ * is not used, whatever its bits.
+ * q_heads % kv_heads == 0, scale finite and > 0, pages * kv_heads * page < 2^31, width * page <= 2^30,
+ * rows <= 2^20, rows * (width * page / 64 + 1) < 2^31.  Scores, softmax and sums are fp32 (LORY_BF16: products on the matrix cores; the probabilities
+ * enter them as two bf16 terms).  Results do not depend on the order in which
+ * workgroups run.
+ * workspace: lory_paged_attn_workspace_bytes(shape); contents undefined before
+ * and after a call.
+ */
+typedef struct {
+    int32_t rows, q_heads, kv_heads, head_dim;
+    int32_t pages, page, width;
+    int32_t dtype;
+    int64_t table_row;
+    float scale;
+} lory_paged_shape;
+int lory_paged_attn_workspace_bytes(const lory_paged_shape *shape, size_t *bytes_out);
+int lory_paged_attn(const lory_paged_shape *shape, const lory_heads *q, const void *k_cache, const void *v_cache,
+                    const int32_t *table, const int32_t *lens, const lory_heads *out, float *lse,
+                    void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -21,13 +21,16 @@ LIB_PATH = os.path.join(_HERE, "liblory.so")
 
 LORY_OK = 0
 LORY_ERR_NULL, LORY_ERR_SHAPE, LORY_ERR_DTYPE, LORY_ERR_ALIGN, LORY_ERR_WORKSPACE, LORY_ERR_DEVICE = range(1, 7)
+LORY_ERR_OVERLAP = 7
 LORY_F32, LORY_BF16 = 0, 1
 LORY_PASS_FWD, LORY_PASS_BWD, LORY_PASS_DENSE = 0, 1, 2
 
 EXPORTS = ("lory_status_string", "lory_version", "lory_set_slab_budget", "lory_set_fused_merge", "lory_profile_enable",
            "lory_profile_read", "lory_merged_save_bytes", "lory_workspace_bytes", "lory_route",
            "lory_route_bwd", "lory_merged_ffn_fwd", "lory_merged_ffn_bwd", "lory_prompt_merge",
-           "lory_dense_ffn_fwd", "lory_dense_ffn_fwd_static")
+           "lory_dense_ffn_fwd", "lory_dense_ffn_fwd_static", "lory_qk_rope", "lory_qk_rope_cache",
+           "lory_qk_rope_workspace_bytes", "lory_qk_rope_bwd", "lory_kv_plan", "lory_paged_attn_workspace_bytes",
+           "lory_paged_attn")
 
 
 class LoryShape(ctypes.Structure):
@@ -39,6 +42,28 @@ class LoryShape(ctypes.Structure):
 class LoryKernelStat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 32), ("launches", ctypes.c_int32), ("ms", ctypes.c_double),
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double)]
+
+
+class LoryHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class LoryRopeShape(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class LoryPlanShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("width", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("free_size", ctypes.c_int32), ("room", ctypes.c_int32), ("table_row", ctypes.c_int64)]
+
+
+class LoryPagedShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("pages", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("dtype", ctypes.c_int32), ("table_row", ctypes.c_int64),
+                ("scale", ctypes.c_float)]
 
 
 class LoryError(RuntimeError):
@@ -89,6 +114,23 @@ def lib() -> ctypes.CDLL:
         L.lory_merged_ffn_fwd.restype = ci
         L.lory_merged_ffn_bwd.argtypes = [sp] + [vp] * 13 + [ci, ci, vp, vp, sz, vp]
         L.lory_merged_ffn_bwd.restype = ci
+        hp, rp = ctypes.POINTER(LoryHeads), ctypes.POINTER(LoryRopeShape)
+        pp, ap = ctypes.POINTER(LoryPlanShape), ctypes.POINTER(LoryPagedShape)
+        i32 = ctypes.c_int32
+        L.lory_qk_rope.argtypes = [rp, hp, hp, vp, vp, vp, vp, hp, hp, vp]
+        L.lory_qk_rope.restype = ci
+        L.lory_qk_rope_cache.argtypes = [rp, hp, hp, hp, vp, vp, vp, vp, hp, vp, vp, i32, i32, vp, vp]
+        L.lory_qk_rope_cache.restype = ci
+        L.lory_qk_rope_workspace_bytes.argtypes = [rp, ctypes.POINTER(sz)]
+        L.lory_qk_rope_workspace_bytes.restype = ci
+        L.lory_qk_rope_bwd.argtypes = [rp, hp, hp, hp, hp, vp, vp, vp, vp, hp, hp, vp, vp, vp, sz, vp]
+        L.lory_qk_rope_bwd.restype = ci
+        L.lory_kv_plan.argtypes = [pp] + [vp] * 12
+        L.lory_kv_plan.restype = ci
+        L.lory_paged_attn_workspace_bytes.argtypes = [ap, ctypes.POINTER(sz)]
+        L.lory_paged_attn_workspace_bytes.restype = ci
+        L.lory_paged_attn.argtypes = [ap, hp, vp, vp, vp, vp, hp, vp, vp, sz, vp]
+        L.lory_paged_attn.restype = ci
         _lib = L
     return _lib
 
@@ -343,3 +385,203 @@ def lory_merged_ffn_bwd(X: torch.Tensor, w: torch.Tensor, Wg: torch.Tensor, Wu: 
                                      _ptr(workspace), workspace.numel(), _stream()),
            "lory_merged_ffn_bwd")
     return dX, dWg, dWu, dWd, dw
+
+
+# ---- the attention half: strided heads, a paged key-value cache
+
+
+def _heads(t: torch.Tensor, like: torch.Tensor, shape: Tuple[int, int, int], name: str) -> LoryHeads:
+    """A [tokens, heads, head_dim] tensor as it lies; only its last index has to be contiguous."""
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}")
+    token, head, last = t.stride()
+    if last != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    return LoryHeads(t.data_ptr(), token, head)
+
+
+def _array(t: torch.Tensor, dtype: torch.dtype, n: int, name: str) -> int:
+    """Address of a contiguous array of n elements."""
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{name} must be {dtype} [{n}]")
+    return _ptr(t)
+
+
+def _table(t: torch.Tensor, rows: int) -> int:
+    if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"table must be int32 [{rows}, width] with contiguous rows")
+    if not t.is_cuda:
+        raise ValueError("table must live on the GPU")
+    return t.data_ptr()
+
+
+def _table_row(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _rope_shape(q: torch.Tensor, k: torch.Tensor, rot: int, eps: float, interleaved: bool) -> LoryRopeShape:
+    n, Hq, D = q.shape
+    return LoryRopeShape(n, Hq, k.shape[1], D, rot, int(interleaved), _dtype_code(q.dtype), eps)
+
+
+def _rope_args(q, k, pos, freq, wq, wk):
+    """Addresses of what the three calls share."""
+    n, Hq, D = q.shape
+    w = []
+    for name, t in (("wq", wq), ("wk", wk)):
+        if t is not None and t.dtype != q.dtype:
+            raise TypeError(f"{name} must be {q.dtype}")
+        w.append(None if t is None else _array(t, q.dtype, D, name))
+    return (_heads(q, q, (n, Hq, D), "q"), _heads(k, q, (n, k.shape[1], D), "k"), _array(pos, torch.int32, n, "pos"),
+            _array(freq, torch.float64, freq.shape[0], "freq"), w[0], w[1])
+
+
+def lory_qk_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, freq: torch.Tensor,
+                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                 wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 interleaved: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Head norms with weights wq, wk [head_dim] (none without them) and position rotation of q [tokens, q_heads,
+    head_dim] and k [tokens, kv_heads, head_dim]; pos [tokens] int32, freq [rot_dim/2] fp64 radians per
+    position.  Returns (q_out, k_out); an output may be its own input."""
+    hq, hk, ppos, pfreq, pwq, pwk = _rope_args(q, k, pos, freq, wq, wk)
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    shape = _rope_shape(q, k, 2 * freq.shape[0], eps, interleaved)
+    _check(lib().lory_qk_rope(shape, hq, hk, ppos, pfreq, pwq, pwk, _heads(q_out, q, q.shape, "q_out"),
+                              _heads(k_out, q, k.shape, "k_out"), _stream()), "lory_qk_rope")
+    return q_out, k_out
+
+
+def _cache_dims(k_cache: torch.Tensor, v_cache: torch.Tensor, like: torch.Tensor, Hkv: int, D: int) -> Tuple[int, int]:
+    pages, heads, page, dim = k_cache.shape
+    if heads != Hkv or dim != D or v_cache.shape != k_cache.shape:
+        raise ValueError(f"k_cache and v_cache must be [pages, {Hkv}, page, {D}]")
+    if k_cache.dtype != like.dtype or v_cache.dtype != like.dtype:
+        raise TypeError(f"k_cache and v_cache must be {like.dtype}")
+    return pages, page
+
+
+def lory_qk_rope_cache(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, freq: torch.Tensor,
+                       k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor,
+                       q_out: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None,
+                       wk: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False) -> torch.Tensor:
+    """lory_qk_rope whose keys go, with the values v beside them, to slots [tokens] int64 of the caches [pages, kv_heads,
+    page, head_dim] (slot = page number * page + row; outside of them: not stored).  Returns q_out."""
+    hq, hk, ppos, pfreq, pwq, pwk = _rope_args(q, k, pos, freq, wq, wk)
+    n, Hkv, D = k.shape
+    pages, page = _cache_dims(k_cache, v_cache, q, Hkv, D)
+    if q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    shape = _rope_shape(q, k, 2 * freq.shape[0], eps, interleaved)
+    _check(lib().lory_qk_rope_cache(shape, hq, hk, _heads(v, q, k.shape, "v"), ppos, pfreq, pwq, pwk,
+                                    _heads(q_out, q, q.shape, "q_out"), _ptr(k_cache), _ptr(v_cache), pages, page,
+                                    _array(slots, torch.int64, n, "slots"), _stream()), "lory_qk_rope_cache")
+    return q_out
+
+
+def lory_qk_rope_workspace_bytes(shape: LoryRopeShape) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().lory_qk_rope_workspace_bytes(shape, ctypes.byref(out)), "lory_qk_rope_workspace_bytes")
+    return out.value
+
+
+def alloc_qk_rope_workspace(q: torch.Tensor, k: torch.Tensor) -> torch.Tensor:
+    """Workspace of lory_qk_rope_bwd for heads of these shapes."""
+    n = lory_qk_rope_workspace_bytes(_rope_shape(q, k, 0, 0.0, False))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=q.device)
+
+
+def lory_qk_rope_bwd(q: torch.Tensor, k: torch.Tensor, dq_out: torch.Tensor, dk_out: torch.Tensor, pos: torch.Tensor,
+                     freq: torch.Tensor, wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None,
+                     eps: float = 1e-6, interleaved: bool = False, dq: Optional[torch.Tensor] = None,
+                     dk: Optional[torch.Tensor] = None, dwq: Optional[torch.Tensor] = None,
+                     dwk: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(dq, dk, dwq, dwk) of lory_qk_rope from the gradients of its outputs; dwq, dwk [head_dim] fp32, None without weights.
+    dq and dk may be dq_out and dk_out."""
+    hq, hk, ppos, pfreq, pwq, pwk = _rope_args(q, k, pos, freq, wq, wk)
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if dk is None:
+        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    D = q.shape[2]
+    if wq is not None:
+        if dwq is None:
+            dwq = torch.empty(D, dtype=torch.float32, device=q.device)
+        if dwk is None:
+            dwk = torch.empty(D, dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = alloc_qk_rope_workspace(q, k)
+    elif dwq is not None or dwk is not None:
+        raise ValueError("dwq and dwk need wq and wk")
+    shape = _rope_shape(q, k, 2 * freq.shape[0], eps, interleaved)
+    _check(lib().lory_qk_rope_bwd(shape, hq, hk, _heads(dq_out, q, q.shape, "dq_out"), _heads(dk_out, q, k.shape, "dk_out"),
+                                  ppos, pfreq, pwq, pwk, _heads(dq, q, q.shape, "dq"), _heads(dk, q, k.shape, "dk"),
+                                  None if dwq is None else _array(dwq, torch.float32, D, "dwq"),
+                                  None if dwk is None else _array(dwk, torch.float32, D, "dwk"), _ptr(workspace),
+                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()),
+           "lory_qk_rope_bwd")
+    return dq, dk, dwq, dwk
+
+
+def lory_kv_plan(lens: torch.Tensor, add: torch.Tensor, table: torch.Tensor, free: torch.Tensor, count: torch.Tensor,
+                 page: int, lens_new: torch.Tensor, cu: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
+                 count_new: torch.Tensor, status: torch.Tensor) -> torch.Tensor:
+    """Pages, positions and slots of a step's new tokens from the rows' lengths (add < 0: the row has ended), and the
+    pages that come back; int32 but slots (int64).  Returns status [1]: 0, or why nothing was planned (include/lory.h)."""
+    B = lens.shape[0]
+    i32 = torch.int32
+    room = positions.shape[0]
+    ptable = _table(table, B)
+    shape = LoryPlanShape(B, table.shape[1], page, free.shape[0], room, _table_row(table))
+    _check(lib().lory_kv_plan(shape, _array(lens, i32, B, "lens"), _array(add, i32, B, "add"), ptable,
+                              _array(free, i32, free.shape[0], "free"), _array(count, i32, 1, "count"),
+                              _array(lens_new, i32, B, "lens_new"), _array(cu, i32, B + 1, "cu"),
+                              _array(positions, i32, room, "positions"), _array(slots, torch.int64, room, "slots"),
+                              _array(count_new, i32, 1, "count_new"), _array(status, i32, 1, "status"), _stream()),
+           "lory_kv_plan")
+    return status
+
+
+def _paged_shape(q: torch.Tensor, k_cache: torch.Tensor, table: torch.Tensor, scale: float) -> LoryPagedShape:
+    B, Hq, D = q.shape
+    pages, Hkv, page, _ = k_cache.shape
+    return LoryPagedShape(B, Hq, Hkv, D, pages, page, table.shape[1], _dtype_code(q.dtype), _table_row(table), scale)
+
+
+def lory_paged_attn_workspace_bytes(shape: LoryPagedShape) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().lory_paged_attn_workspace_bytes(shape, ctypes.byref(out)), "lory_paged_attn_workspace_bytes")
+    return out.value
+
+
+def alloc_paged_attn_workspace(q: torch.Tensor, k_cache: torch.Tensor, table: torch.Tensor) -> torch.Tensor:
+    """Workspace of lory_paged_attn for these shapes."""
+    n = lory_paged_attn_workspace_bytes(_paged_shape(q, k_cache, table, 1.0))
+    return torch.empty(n, dtype=torch.uint8, device=q.device)
+
+
+def lory_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
+    """out [rows, q_heads, head_dim] = attention of one token per row, q, over the first lens[b] tokens that table [rows,
+    width] finds in the caches [pages, kv_heads, page, head_dim]; lse [rows, q_heads] fp32 receives the log of
+    the sum of exponentials.  scale is 1/sqrt(head_dim) unless given."""
+    B, Hq, D = q.shape
+    _cache_dims(k_cache, v_cache, q, k_cache.shape[1], D)
+    shape = _paged_shape(q, k_cache, table, D ** -0.5 if scale is None else scale)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if workspace is None:
+        workspace = alloc_paged_attn_workspace(q, k_cache, table)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, Hq)):
+        raise ValueError(f"lse must be fp32 [{B}, {Hq}]")
+    _check(lib().lory_paged_attn(shape, _heads(q, q, q.shape, "q"), _ptr(k_cache), _ptr(v_cache), _table(table, B),
+                                 _array(lens, torch.int32, B, "lens"), _heads(out, q, q.shape, "out"), _ptr(lse),
+                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()), "lory_paged_attn")
+    return out

@@ -52,6 +52,7 @@ const char *lory_status_string(int status)
     case LORY_ERR_ALIGN: return "pointer is not 16-byte aligned";
     case LORY_ERR_WORKSPACE: return "workspace too small";
     case LORY_ERR_DEVICE: return "HIP call or kernel launch failed";
+    case LORY_ERR_OVERLAP: return "an output overlaps another buffer of the call";
     default: return "unknown status";
     }
 }

@@ -44,7 +44,7 @@ inline int launch_status()
 namespace prof {
 enum Class { kRoute = 0, kMerge, kGemmGU, kSwigluFwd, kGemmDown, kGemmDA, kSwigluBwd, kGemmDX, kGemmDWGU, kGemmDWD, kScatter,
              kDwReduce, kRouteBwd, kDenseSkinny, kFusedGU, kFusedDown, kFusedDA, kFusedDX, kFusedDW,
-             kNumClasses };
+             kQkRope, kQkRopeBwd, kKvPlan, kPagedAttn, kNumClasses };
 bool enabled();
 int set_enabled(int on);
 int read(lory_kernel_stat *out, int max_out, int *n_out);
@@ -146,5 +146,27 @@ int bf16_ffn_bwd(const Dims &m, const void *X, const float *w, const void *Wg, c
                  const void *Wd, const void *dY, const void *G_save, const void *U_save,
                  const void *Wbar_save, void *dX, void *dWg, void *dWu, void *dWd, int grad_dtype,
                  int accumulate, float *dw, void *ws, hipStream_t st);
+
+// ---- operators of the attention half (qk_rope.hip, qk_rope_bwd.hip, kv_plan.hip, paged_attn.hip); arguments are checked
+struct RopeCache {
+    const lory_heads *v;
+    void *k_cache, *v_cache;
+    int pages, page;
+    const int64_t *slots;
+};
+// k_out or cache: where the keys go
+int qk_rope_launch(const lory_rope_shape &s, const lory_heads &q, const lory_heads &k, const int32_t *pos, const double *freq,
+                   const void *wq, const void *wk, const lory_heads &q_out, const lory_heads *k_out, const RopeCache *cache,
+                   hipStream_t st);
+size_t qk_rope_bwd_workspace_bytes(const lory_rope_shape &s);
+int qk_rope_bwd_launch(const lory_rope_shape &s, const lory_heads &q, const lory_heads &k, const lory_heads &dq_out,
+                       const lory_heads &dk_out, const int32_t *pos, const double *freq, const void *wq, const void *wk,
+                       const lory_heads &dq, const lory_heads &dk, float *dwq, float *dwk, void *ws, hipStream_t st);
+int kv_plan_launch(const lory_plan_shape &s, const int32_t *lens, const int32_t *add, int32_t *table, int32_t *free,
+                   const int32_t *count, int32_t *lens_new, int32_t *cu, int32_t *positions, int64_t *slots, int32_t *count_new,
+                   int32_t *status, hipStream_t st);
+size_t paged_attn_workspace_bytes(const lory_paged_shape &s);
+int paged_attn_launch(const lory_paged_shape &s, const lory_heads &q, const void *k_cache, const void *v_cache,
+                      const int32_t *table, const int32_t *lens, const lory_heads &out, float *lse, void *ws, hipStream_t st);
 
 }  // namespace lory

@@ -1,0 +1,544 @@
+// Attention of one new token per row over a paged key-value cache (lory_paged_attn).
+//
+// Bound by the bytes of the cache: every key and value is read once, for all query heads that share it.
+//
+// Work.  A unit is kTile keys of one key-value head of one row (of up to 16 of its query heads).  The units of all rows
+// and heads, in order, are cut into as many equal ranges as there are workgroups, whatever the rows' lengths, which only
+// the device knows: every workgroup takes the sums over the lengths for itself.  A range ends inside a row's units as it
+// comes; such a piece leaves its maximum, sum and unnormalised output in the workspace (at most two pieces a workgroup:
+// the first and the last), and a second launch joins the pieces of a row in order.  Rows that lie in one range are written directly.
+//
+// A wavefront takes 32 (bf16) or 16 (fp32) keys at a time, straight from memory to the operands of the matrix cores:
+//   S^T [keys x queries] = K Q^T   A = K: lane (i, c) holds pieces of 16 bytes of key i
+//   O^T [dims x queries] += V^T P^T
+// S^T leaves a lane with the scores of its query (column i) and of keys 4c .. 4c+3, which is the layout of P^T as the
+// other product's operand if its keys are taken in that order, so the probabilities never move between lanes.  V rows are
+// read whole by 16 lanes; lane i holds dims nt i .. nt i + nt - 1 of eight keys, and a v_perm per pair of keys gives the operand of
+// one matrix instruction per dim: row i of output tile t is dim nt i + t.  fp32 needs no transposition (one key per lane and instruction).
+// The probabilities go in as two bf16 terms (p = hi + lo, error 2^-18): one alone would round every weight of the sum to
+// 2^-9, and the matrix cores wait for memory anyway.
+//
+// Pages: the lane that owns a key looks its page up two steps ahead; the others fetch the row by a lane permute.
+#include "gemm_bf16.h"
+#include "lory_internal.h"
+
+#include "elem_io.h"
+#include "paged_index.h"
+
+namespace lory {
+
+namespace {
+
+using gemm::bf16x8;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kGroups = 512;   // workgroups: two on each of 256 CUs
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Args {
+    const char *q;
+    long q_row, q_head;   // bytes
+    const char *k, *v;
+    const int32_t *table;
+    long table_row;
+    const int32_t *lens;
+    char *out;
+    long out_row, out_head;   // bytes
+    float *lse;
+    int32_t *starts;          // workspace: units of one head before each row, [rows + 1]
+    float *part_o, *part_ml;  // pieces: [2 * kGroups][16][D] and [2 * kGroups][16][2]
+    int rows, Hq, Hkv, D, pages, page, width;
+    int group, tiles;         // query heads of a key-value head, and blocks of 16 of them
+    paged::Divider div;       // by page
+    float scale2;             // scale * log2(e)
+};
+
+template <typename T> constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;   // of a wavefront's step
+template <typename T> constexpr int kTile = kKeys<T> * kWaves;
+
+__device__ __forceinline__ int length_of(const Args &a, int b)
+{
+    const int n = a.lens[b], most = a.width * a.page;
+    return n < 0 ? 0 : n < most ? n : most;
+}
+
+template <typename T> __device__ __forceinline__ int units_of(int len)
+{
+    return len <= kTile<T> ? 1 : (len + kTile<T> - 1) / kTile<T>;   // an empty row has one, which writes its zeros
+}
+
+__device__ __forceinline__ int owner(long u, long U) { return paged::owner(u, U, kGroups); }
+__device__ __forceinline__ long range_begin(int w, long U) { return paged::range_begin(w, U, kGroups); }
+
+__device__ __forceinline__ float xor_max(float v)
+{
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float xor_sum(float v)
+{
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+
+// One row's head for one wavefront: the operand of Q, the running softmax and the output.
+// DP: head_dim rounded up to 64, 128 or 256.  PAD: head_dim < DP (pieces behind it are zeros that nothing loads).
+template <typename T, int DP, bool PAD> struct Wave;
+
+template <int DP, bool PAD> struct Wave<__hip_bfloat16, DP, PAD> {
+    static constexpr int KS = DP / 32;     // K steps of a product over the dims
+    static constexpr int NT = DP / 16;     // output tiles
+    static constexpr int VW = NT < 8 ? NT : 8;   // dims of a V load
+    static constexpr int VL = NT / VW;     // V loads of a key
+    bf16x8 q[KS];
+    u32x4 k[2][KS];
+    uint32_t v[8][VL][VW / 2];
+    f32x4 o[NT];
+
+    // dim of row i of output tile t
+    static __device__ int dim(int t, int i) { return (t / VW) * 16 * VW + VW * i + t % VW; }
+
+    __device__ void load_q(const char *p, int D, int c, bool on)
+    {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            u32x4 r = {0, 0, 0, 0};
+            if (on && (!PAD || (4 * s + c) * 8 < D)) r = *reinterpret_cast<const u32x4 *>(p + (4 * s + c) * 16);
+            q[s] = __builtin_bit_cast(bf16x8, r);
+        }
+    }
+    // row: of the lane's own key of the step (lane & 31)
+    __device__ void load_k(const char *base, int row, int D, int i, int c)
+    {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            const long r = __shfl(row, kt * 16 + i, 64);
+            const char *p = base + r * (D * 2) + c * 16;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                if (PAD) k[kt][s] = u32x4{0, 0, 0, 0};
+                if (!PAD || (4 * s + c) * 8 < D) k[kt][s] = *reinterpret_cast<const u32x4 *>(p + s * 64);
+            }
+        }
+    }
+    __device__ void load_v(const char *base, int row, int D, int i, int c)
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const long r = __shfl(row, (j >> 2) * 16 + 4 * c + (j & 3), 64);
+            const char *p = base + r * (D * 2) + i * (VW * 2);
+#pragma unroll
+            for (int m = 0; m < VL; ++m) {
+                if constexpr (VW == 8) {
+                    u32x4 x = {0, 0, 0, 0};
+                    if (!PAD || (16 * m + i) * 8 < D) x = *reinterpret_cast<const u32x4 *>(p + m * 256);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[j][m][e] = x[e];
+                } else {
+                    uint2 x = {0, 0};
+                    if (!PAD || i * 4 < D) x = *reinterpret_cast<const uint2 *>(p);
+                    v[j][m][0] = x.x;
+                    v[j][m][1] = x.y;
+                }
+            }
+        }
+    }
+    // s[n]: score of the lane's query with key (n / 4) * 16 + 4c + n % 4
+    __device__ void scores(float (&s)[8])
+    {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int t = 0; t < KS; ++t)
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[kt][t]), q[t], acc, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[kt * 4 + r] = acc[r];
+        }
+    }
+    // the values of keys that are left out have no bits that may enter a product
+    __device__ void clear_v(uint32_t valid, int c)
+    {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool on = (valid >> ((j >> 2) * 16 + 4 * c + (j & 3))) & 1;
+#pragma unroll
+            for (int m = 0; m < VL; ++m)
+#pragma unroll
+                for (int e = 0; e < VW / 2; ++e) v[j][m][e] = on ? v[j][m][e] : 0;
+        }
+    }
+    __device__ void add(const float (&p)[8])
+    {
+        u32x4 hi, lo;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            hi[n] = gemm::cvt_pk_bf16(p[2 * n], p[2 * n + 1]);
+            lo[n] = gemm::cvt_pk_bf16(p[2 * n] - __uint_as_float(hi[n] << 16), p[2 * n + 1] - __uint_as_float(hi[n] & 0xffff0000u));
+        }
+        const bf16x8 bh = __builtin_bit_cast(bf16x8, hi), bl = __builtin_bit_cast(bf16x8, lo);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            u32x4 x;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                x[n] = __builtin_amdgcn_perm(v[2 * n + 1][t / VW][(t % VW) / 2], v[2 * n][t / VW][(t % VW) / 2],
+                                             (t & 1) ? 0x07060302u : 0x05040100u);
+            const bf16x8 af = __builtin_bit_cast(bf16x8, x);
+            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af, bh, o[t], 0, 0, 0);
+            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af, bl, o[t], 0, 0, 0);
+        }
+    }
+};
+
+template <int DP, bool PAD> struct Wave<float, DP, PAD> {
+    static constexpr int KS = DP / 16;   // 16-byte pieces of a key per lane
+    static constexpr int NT = DP / 16;
+    static constexpr int VL = DP / 64;
+    f32x4 q[KS];
+    f32x4 k[KS];
+    f32x4 v[4][VL];
+    f32x4 o[NT];
+
+    static __device__ int dim(int t, int i) { return (t / 4) * 64 + 4 * i + t % 4; }
+
+    __device__ void load_q(const char *p, int D, int c, bool on)
+    {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            q[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (on && (!PAD || (4 * s + c) * 4 < D)) q[s] = *reinterpret_cast<const f32x4 *>(p + (4 * s + c) * 16);
+        }
+    }
+    __device__ void load_k(const char *base, int row, int D, int i, int c)
+    {
+        const long r = __shfl(row, i, 64);
+        const char *p = base + r * (D * 4) + c * 16;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            if (PAD) k[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (!PAD || (4 * s + c) * 4 < D) k[s] = *reinterpret_cast<const f32x4 *>(p + s * 64);
+        }
+    }
+    __device__ void load_v(const char *base, int row, int D, int i, int c)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const long r = __shfl(row, 4 * c + j, 64);
+            const char *p = base + r * (D * 4) + i * 16;
+#pragma unroll
+            for (int m = 0; m < VL; ++m) {
+                if (PAD) v[j][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (!PAD || (16 * m + i) * 4 < D) v[j][m] = *reinterpret_cast<const f32x4 *>(p + m * 256);
+            }
+        }
+    }
+    __device__ void scores(float (&s)[4])
+    {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < KS; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][e], q[t][e], acc, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[r] = acc[r];
+    }
+    __device__ void clear_v(uint32_t valid, int c)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const bool on = (valid >> (4 * c + j)) & 1;
+#pragma unroll
+            for (int m = 0; m < VL; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[j][m][e] = on ? v[j][m][e] : 0.f;
+        }
+    }
+    __device__ void add(const float (&p)[4])
+    {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][t / 4][t % 4], p[j], o[t], 0, 0, 0);
+    }
+};
+
+template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Args a)
+{
+    using W = Wave<T, DP, PAD>;
+    constexpr int KEYS = kKeys<T>, TILE = kTile<T>, NS = KEYS / 4;
+    constexpr int LD = DP + 4;   // row of the LDS copy of a wavefront's output
+    __shared__ float so[kWaves][16][LD];
+    __shared__ float sm[kWaves][16], sl[kWaves][16];
+    __shared__ int sums[kThreads + 1], wsum[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, c = lane >> 4;
+    const int heads = a.Hkv * a.tiles;
+
+    // units of one head before each chunk of rows
+    const int chunk = (a.rows + kThreads - 1) / kThreads;
+    {
+        int n = 0;
+        for (int b = tid * chunk; b < min((tid + 1) * chunk, a.rows); ++b) n += units_of<T>(length_of(a, b));
+        for (int m = 1; m < 64; m <<= 1) {
+            const int u = __shfl_up(n, m, 64);
+            if (lane >= m) n += u;
+        }
+        if (lane == 63) wsum[wave] = n;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) n += wsum[w];
+        sums[tid + 1] = n;
+        if (tid == 0) sums[0] = 0;
+        __syncthreads();
+    }
+    if (blockIdx.x == 0) {   // for the launch that joins
+        int n = sums[tid];
+        for (int b = tid * chunk; b < min((tid + 1) * chunk, a.rows); ++b) {
+            a.starts[b] = n;
+            n += units_of<T>(length_of(a, b));
+        }
+        if (tid == 0) a.starts[a.rows] = sums[kThreads];
+    }
+    const long U = (long)sums[kThreads] * heads;
+    long u = range_begin(blockIdx.x, U);
+    const long end = range_begin(blockIdx.x + 1, U);
+    if (u >= end) return;
+
+    // row, head and tile of the first unit
+    int b, h, tile, len, units;
+    {
+        int lo = 0, hi = kThreads;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((long)sums[mid] * heads <= u) lo = mid; else hi = mid;
+        }
+        b = lo * chunk;
+        long rest = u - (long)sums[lo] * heads;
+        for (;; ++b) {
+            len = length_of(a, b);
+            units = units_of<T>(len);
+            if (rest < (long)units * heads || b == a.rows - 1) break;
+            rest -= (long)units * heads;
+        }
+        h = (int)(rest / units);
+        tile = (int)(rest - (long)h * units);
+    }
+
+    W w;
+    while (u < end) {
+        const int stop = (int)(end - u < units - tile ? tile + (end - u) : units);
+        const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;   // first query head
+        const int nq = min(16, (kvh + 1) * a.group - first);
+        const int last = min(stop * TILE, len);
+
+        w.load_q(a.q + b * a.q_row + (first + i) * a.q_head, a.D, c, i < nq);
+#pragma unroll
+        for (int t = 0; t < W::NT; ++t) w.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+
+        // page of the lane's key of the step at `at`, -1 where there is none
+        const int32_t *pages = a.table + b * a.table_row;
+        auto page_of = [&](int at) {
+            const int t = at + (lane & (KEYS - 1));
+            return t < last ? pages[paged::quotient(a.div, t)] : -1;
+        };
+        auto row_of = [&](int at, int page) {
+            return paged::cache_row(a.div, at + (lane & (KEYS - 1)), page, a.pages, a.Hkv, kvh);
+        };
+        int at = tile * TILE + wave * KEYS;
+        int row = row_of(at, page_of(at)), next = page_of(at + TILE);
+        if (at < last) {
+            w.load_k(a.k, max(row, 0), a.D, i, c);
+            w.load_v(a.v, max(row, 0), a.D, i, c);
+        }
+        for (; at < last; at += TILE) {
+            const uint32_t valid = (uint32_t)__ballot(row >= 0);
+            const int row1 = row_of(at + TILE, next);
+            next = page_of(at + 2 * TILE);
+            const bool more = at + TILE < last;
+
+            float s[NS];
+            w.scores(s);
+            if (more) w.load_k(a.k, max(row1, 0), a.D, i, c);
+
+            float top = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                s[n] = (valid >> ((n >> 2) * 16 + 4 * c + (n & 3))) & 1 ? s[n] * a.scale2 : -INFINITY;
+                top = fmaxf(top, s[n]);
+            }
+            const float m1 = fmaxf(m, xor_max(top));
+            const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing but -inf so far: every weight is 0
+            if (__any(m1 != m)) {
+                const float f = exp2f(m - ref);
+                l *= f;
+#pragma unroll
+                for (int t = 0; t < W::NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) w.o[t][r] *= f;
+            }
+            m = m1;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                s[n] = exp2f(s[n] - ref);
+                l += s[n];
+            }
+            if (valid != (uint32_t)((1ull << KEYS) - 1)) w.clear_v(valid, c);
+            w.add(s);
+            if (more) w.load_v(a.v, max(row1, 0), a.D, i, c);
+            row = row1;
+        }
+        l = xor_sum(l);
+
+        // the four wavefronts together
+        if (c == 0) {
+            sm[wave][i] = m;
+            sl[wave][i] = l;
+        }
+        if (i < nq) {
+#pragma unroll
+            for (int t = 0; t < W::NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) so[wave][i][W::dim(t, 4 * c + r)] = w.o[t][r];
+        }
+        __syncthreads();
+        const bool whole = tile == 0 && stop == units;
+        const int slot = 2 * blockIdx.x + (tile == 0 ? 1 : 0);
+        for (int x = tid; x < nq * a.D; x += kThreads) {
+            const int j = x / a.D, d = x - j * a.D;
+            float M = sm[0][j];
+#pragma unroll
+            for (int n = 1; n < kWaves; ++n) M = fmaxf(M, sm[n][j]);
+            const float ref = M == -INFINITY ? 0.f : M;
+            float L = 0.f, O = 0.f;
+#pragma unroll
+            for (int n = 0; n < kWaves; ++n) {
+                const float f = exp2f(sm[n][j] - ref);
+                L = fmaf(f, sl[n][j], L);
+                O = fmaf(f, so[n][j][d], O);
+            }
+            if (whole) {
+                Elem<T>::store((T *)(a.out + b * a.out_row + (first + j) * a.out_head) + d, O / (L == 0.f ? 1.f : L));
+                if (d == 0 && a.lse) a.lse[(long)b * a.Hq + first + j] = (ref + log2f(L)) * kLn2;
+            } else {
+                a.part_o[((long)slot * 16 + j) * a.D + d] = O;
+                if (d == 0) {
+                    a.part_ml[(slot * 16 + j) * 2] = M;
+                    a.part_ml[(slot * 16 + j) * 2 + 1] = L;
+                }
+            }
+        }
+        __syncthreads();
+
+        u += stop - tile;
+        tile = 0;
+        if (stop == units && ++h == heads && u < end) {
+            h = 0;
+            ++b;
+            len = length_of(a, b);
+            units = units_of<T>(len);
+        }
+    }
+}
+
+// Joins the pieces of one row's head: grid (heads, rows).
+template <typename T> __global__ __launch_bounds__(kThreads) void paged_attn_join_kernel(Args a)
+{
+    const int h = blockIdx.x, heads = gridDim.x;
+    for (int b = blockIdx.y; b < a.rows; b += gridDim.y) {
+        const long U = (long)a.starts[a.rows] * heads;
+        const int units = a.starts[b + 1] - a.starts[b];
+        const long u0 = (long)a.starts[b] * heads + (long)h * units, u1 = u0 + units;
+        const int w0 = owner(u0, U), w1 = owner(u1 - 1, U);
+        if (w0 == w1) continue;   // written already
+        const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;
+        const int nq = min(16, (kvh + 1) * a.group - first);
+        for (int x = threadIdx.x; x < nq * a.D; x += kThreads) {
+            const int j = x / a.D, d = x - j * a.D;
+            float M = -INFINITY, L = 0.f, O = 0.f;
+            for (int w = w0; w <= w1; ++w) {
+                if (range_begin(w, U) == range_begin(w + 1, U)) continue;
+                const int slot = 2 * w + (w == w0 ? 1 : 0);
+                const float m = a.part_ml[(slot * 16 + j) * 2], l = a.part_ml[(slot * 16 + j) * 2 + 1];
+                const float M1 = fmaxf(M, m), ref = M1 == -INFINITY ? 0.f : M1;
+                const float f = exp2f(M - ref), g = exp2f(m - ref);
+                L = L * f + l * g;
+                O = O * f + a.part_o[((long)slot * 16 + j) * a.D + d] * g;
+                M = M1;
+            }
+            Elem<T>::store((T *)(a.out + b * a.out_row + (first + j) * a.out_head) + d, O / (L == 0.f ? 1.f : L));
+            if (d == 0 && a.lse) a.lse[(long)b * a.Hq + first + j] = ((M == -INFINITY ? 0.f : M) + log2f(L)) * kLn2;
+        }
+    }
+}
+
+template <typename T, int DP> void launch2(const Args &a, hipStream_t st)
+{
+    if (a.D == DP)
+        hipLaunchKernelGGL((paged_attn_kernel<T, DP, false>), dim3(kGroups), dim3(kThreads), 0, st, a);
+    else
+        hipLaunchKernelGGL((paged_attn_kernel<T, DP, true>), dim3(kGroups), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL((paged_attn_join_kernel<T>), dim3(a.Hkv * a.tiles, a.rows < 32768 ? a.rows : 32768), dim3(kThreads), 0, st, a);
+}
+
+template <typename T> void launch1(const Args &a, hipStream_t st)
+{
+    if (a.D <= 64)
+        launch2<T, 64>(a, st);
+    else if (a.D <= 128)
+        launch2<T, 128>(a, st);
+    else
+        launch2<T, 256>(a, st);
+}
+
+size_t starts_bytes(const lory_paged_shape &s) { return align_up(((size_t)s.rows + 1) * sizeof(int32_t), 256); }
+
+}  // namespace
+
+size_t paged_attn_workspace_bytes(const lory_paged_shape &s)
+{
+    return align_up(starts_bytes(s) + (size_t)2 * kGroups * 16 * (s.head_dim + 2) * sizeof(float), 256);
+}
+
+int paged_attn_launch(const lory_paged_shape &s, const lory_heads &q, const void *k_cache, const void *v_cache,
+                      const int32_t *table, const int32_t *lens, const lory_heads &out, float *lse, void *ws, hipStream_t st)
+{
+    const int esize = s.dtype == LORY_F32 ? 4 : 2;
+    Args a = {};
+    a.q = (const char *)q.data;
+    a.q_row = q.token * esize;
+    a.q_head = q.head * esize;
+    a.k = (const char *)k_cache;
+    a.v = (const char *)v_cache;
+    a.table = table;
+    a.table_row = s.table_row;
+    a.lens = lens;
+    a.out = (char *)out.data;
+    a.out_row = out.token * esize;
+    a.out_head = out.head * esize;
+    a.lse = lse;
+    a.starts = (int32_t *)ws;
+    a.part_o = (float *)((char *)ws + starts_bytes(s));
+    a.part_ml = a.part_o + (size_t)2 * kGroups * 16 * s.head_dim;
+    a.rows = s.rows;
+    a.Hq = s.q_heads;
+    a.Hkv = s.kv_heads;
+    a.D = s.head_dim;
+    a.pages = s.pages;
+    a.page = s.page;
+    a.width = s.width;
+    a.group = s.q_heads / s.kv_heads;
+    a.tiles = (a.group + 15) / 16;
+    a.div = paged::divider(s.page);
+    a.scale2 = s.scale * kLog2e;
+    prof::Range r(st, prof::kPagedAttn, 0.0, 0.0);   // the lengths are on the device
+    if (s.dtype == LORY_F32)
+        launch1<float>(a, st);
+    else
+        launch1<__hip_bfloat16>(a, st);
+    return launch_status();
+}
+
+}  // namespace lory

@@ -31,7 +31,8 @@ int32_t *g_counts = nullptr;   // per record, in host memory that the GPU writes
 const char *const kNames[kNumClasses] = {"route",     "merge",     "gemm_gate_up", "swiglu_fwd", "gemm_down",
                                          "gemm_dA",   "swiglu_bwd", "gemm_dX",   "gemm_dW_gate_up",
                                          "gemm_dW_down", "scatter_dots", "dw_reduce", "route_bwd", "dense_skinny",
-                                         "fused_gate_up", "fused_down", "fused_dA", "fused_dX", "fused_dW_dots"};
+                                         "fused_gate_up", "fused_down", "fused_dA", "fused_dX", "fused_dW_dots",
+                                         "qk_rope", "qk_rope_bwd", "kv_plan", "paged_attn"};
 
 // Events are created when timing is switched on (and by lory_profile_read, which returns
 // them to the pool), never inside a launch: a launch only takes events from the pool and

@@ -1,0 +1,235 @@
+// Gradient of the head norm and rotation (lory_qk_rope_bwd).
+//
+// HBM-bound: heads and their gradients are read once, the input gradients written once.  With g = the gradient turned back,
+//   dx = r g w - x r^3 / D * sum(g w x),   dw += g x r,
+// so both sums of a head (x^2 and g w x) come from the same registers.  Wavefronts walk over tokens and keep dw of their
+// chunk in registers; every workgroup adds its wavefronts in LDS and leaves one row of partial sums, and a second
+// launch adds the rows in order: the same bits on every run.
+#include "qk_rope.h"
+
+namespace lory {
+
+namespace {
+
+using namespace rope;
+
+constexpr int kMaxBlocks = 1024;   // rows of partial sums
+
+struct Args {
+    Heads q, k, dyq, dyk, dq, dk;
+    const int32_t *pos;
+    const double *freq;
+    const void *wq, *wk;
+    float *part;   // [blocks][2][D]
+    int tokens, shares, Hq, Hkv, D, rot;
+    float eps;
+};
+
+template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds__(64 * kWaves) void qk_rope_bwd_kernel(Args a)
+{
+    constexpr int VEC = 16 / sizeof(T), HPW = 64 / LPH, U = 2;
+    __shared__ float2 table[kWaves][kMaxPairs];
+    __shared__ float sums[kWaves][2 * LPH * VEC];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Lane l = lane_of<T, LPH, INTER>(lane, a.D, a.rot);
+    const int gq = (a.Hq + HPW - 1) / HPW, gk = (a.Hkv + HPW - 1) / HPW, groups = gq + gk;
+
+    float accq[VEC], acck[VEC], wq[VEC], wk[VEC];
+    weights<T, INTER>(l, (const T *)a.wq, false, wq);
+    weights<T, INTER>(l, (const T *)a.wk, false, wk);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) accq[e] = acck[e] = 0.f;
+
+    // an item is a share of a token's heads
+    const long items = (long)a.tokens * a.shares;
+    for (long item = (long)blockIdx.x * kWaves + wave; item < items; item += (long)gridDim.x * kWaves) {
+        const int t = (int)(item / a.shares), share = (int)(item - (long)t * a.shares);
+        const int g0 = share * groups / a.shares, g1 = (share + 1) * groups / a.shares;
+        const double pos = a.pos[t];
+        wave_sync();   // the table's last readers are done
+        for (int i = lane; i < (a.rot >> 1); i += 64) table[wave][i] = turn_of(pos, a.freq[i]);
+        wave_sync();
+        float c[VEC], s[VEC];
+        factors<T, INTER>(l, table[wave], -1.f, c, s);
+
+        auto section = [&](int lo, int hi, int H, const char *src, long src_head, const char *grad, long grad_head, char *dst,
+                           long dst_head, const float (&w)[VEC], float (&acc)[VEC]) {
+            for (int g = lo; g < hi; g += U) {
+                Chunk rx[U], rg[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int h = (g + u) * HPW + l.sub;
+                    rx[u] = rg[u] = Chunk{0, 0, 0, 0};
+                    if (g + u < hi && h < H && l.on) {
+                        if constexpr (NORM) rx[u] = *reinterpret_cast<const Chunk *>(src + h * src_head + l.chunk * 16);
+                        rg[u] = *reinterpret_cast<const Chunk *>(grad + h * grad_head + l.chunk * 16);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (g + u >= hi) break;
+                    const int h = (g + u) * HPW + l.sub;
+                    float dy[VEC], p[VEC], y[VEC];
+                    widen<T>(rg[u], dy);
+                    widen<T>(exchange<T, LPH, INTER>(l, rg[u]), p);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) y[e] = fmaf(dy[e], c[e], p[e] * s[e]);
+                    if constexpr (NORM) {
+                        float x[VEC], xx = 0.f, gx = 0.f;
+                        widen<T>(rx[u], x);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            xx = fmaf(x[e], x[e], xx);
+                            gx = fmaf(y[e] * w[e], x[e], gx);
+                        }
+                        const float r = rsqrtf(head_sum<LPH>(xx) / (float)a.D + a.eps);
+                        const float m = head_sum<LPH>(gx) / (float)a.D * r * r;
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            acc[e] = fmaf(y[e], x[e] * r, acc[e]);
+                            y[e] = r * fmaf(-x[e], m, y[e] * w[e]);
+                        }
+                    }
+                    if (h < H && l.on) *reinterpret_cast<Chunk *>(dst + h * dst_head + l.chunk * 16) = narrow<T>(y);
+                }
+            }
+        };
+        section(g0, g1 < gq ? g1 : gq, a.Hq, a.q.p + t * a.q.token, a.q.head, a.dyq.p + t * a.dyq.token, a.dyq.head,
+                a.dq.p + t * a.dq.token, a.dq.head, wq, accq);
+        section((g0 > gq ? g0 : gq) - gq, g1 - gq, a.Hkv, a.k.p + t * a.k.token, a.k.head, a.dyk.p + t * a.dyk.token, a.dyk.head,
+                a.dk.p + t * a.dk.token, a.dk.head, wk, acck);
+    }
+    if constexpr (NORM) {
+        // the heads of a wavefront's groups, then the wavefronts, in order
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+#pragma unroll
+            for (int m = LPH; m < 64; m <<= 1) {
+                accq[e] += __shfl_xor(accq[e], m, 64);
+                acck[e] += __shfl_xor(acck[e], m, 64);
+            }
+            if (l.sub == 0) {
+                sums[wave][l.chunk * VEC + e] = accq[e];
+                sums[wave][(LPH + l.chunk) * VEC + e] = acck[e];
+            }
+        }
+        __syncthreads();
+        float *dst = a.part + (size_t)blockIdx.x * 2 * a.D;
+        for (int i = threadIdx.x; i < 2 * a.D; i += 64 * kWaves) {
+            const int j = i < a.D ? i : i - a.D + LPH * VEC;
+            dst[i] = sums[0][j] + sums[1][j] + sums[2][j] + sums[3][j];
+        }
+    }
+}
+
+// dw from the rows of partial sums: a wavefront of a workgroup takes every 16th row of 64 columns, and the 16 sums are added
+// in order.
+__global__ __launch_bounds__(1024) void qk_rope_dw_kernel(const float *part, int rows, int D, float *dwq, float *dwk)
+{
+    __shared__ float sums[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = blockIdx.x * 64 + lane;
+    float v = 0.f;
+    if (col < 2 * D) {
+#pragma unroll 8
+        for (int r = wave; r < rows; r += 16) v += part[(size_t)r * 2 * D + col];
+    }
+    sums[wave][lane] = v;
+    __syncthreads();
+    if (wave != 0 || col >= 2 * D) return;
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) total += sums[i][lane];
+    (col < D ? dwq : dwk)[col < D ? col : col - D] = total;
+}
+
+struct Plan {
+    int shares, blocks;
+};
+
+// A token's heads over several wavefronts until there are 4096 of them; then several tokens a wavefront.
+Plan plan(const lory_rope_shape &s)
+{
+    const int lph = s.dtype == LORY_F32 ? lanes_per_head<float>(s.head_dim) : lanes_per_head<__hip_bfloat16>(s.head_dim);
+    const int hpw = 64 / lph, groups = (s.q_heads + hpw - 1) / hpw + (s.kv_heads + hpw - 1) / hpw;
+    Plan p = {1, 0};
+    if (s.tokens <= 0) return p;
+    long shares = (4 * kMaxBlocks + (long)s.tokens - 1) / s.tokens;
+    p.shares = (int)(shares < groups ? shares : groups);
+    const long blocks = ((long)s.tokens * p.shares + kWaves - 1) / kWaves;
+    p.blocks = (int)(blocks < kMaxBlocks ? blocks : kMaxBlocks);
+    return p;
+}
+
+template <typename T, int LPH> void launch2(const Args &a, int blocks, bool inter, bool norm, hipStream_t st)
+{
+    const dim3 grid(blocks), block(64 * kWaves);
+    if (inter && norm)
+        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, true, true>), grid, block, 0, st, a);
+    else if (inter)
+        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, true, false>), grid, block, 0, st, a);
+    else if (norm)
+        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, false, true>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, false, false>), grid, block, 0, st, a);
+}
+
+template <typename T> void launch1(const Args &a, int blocks, bool inter, bool norm, hipStream_t st)
+{
+    switch (lanes_per_head<T>(a.D)) {
+    case 8: launch2<T, 8>(a, blocks, inter, norm, st); break;
+    case 16: launch2<T, 16>(a, blocks, inter, norm, st); break;
+    case 32: launch2<T, 32>(a, blocks, inter, norm, st); break;
+    default:
+        if constexpr (sizeof(T) == 4) launch2<T, 64>(a, blocks, inter, norm, st);
+    }
+}
+
+}  // namespace
+
+size_t qk_rope_bwd_workspace_bytes(const lory_rope_shape &s)
+{
+    return align_up((size_t)plan(s).blocks * 2 * s.head_dim * sizeof(float), 256);
+}
+
+int qk_rope_bwd_launch(const lory_rope_shape &s, const lory_heads &q, const lory_heads &k, const lory_heads &dq_out,
+                       const lory_heads &dk_out, const int32_t *pos, const double *freq, const void *wq, const void *wk,
+                       const lory_heads &dq, const lory_heads &dk, float *dwq, float *dwk, void *ws, hipStream_t st)
+{
+    const int esize = s.dtype == LORY_F32 ? 4 : 2;
+    const Plan p = plan(s);
+    Args a = {};
+    a.q = heads(q, esize);
+    a.k = heads(k, esize);
+    a.dyq = heads(dq_out, esize);
+    a.dyk = heads(dk_out, esize);
+    a.dq = heads(dq, esize);
+    a.dk = heads(dk, esize);
+    a.pos = pos;
+    a.freq = freq;
+    a.wq = wq;
+    a.wk = wk;
+    a.part = (float *)ws;
+    a.tokens = s.tokens;
+    a.shares = p.shares;
+    a.Hq = s.q_heads;
+    a.Hkv = s.kv_heads;
+    a.D = s.head_dim;
+    a.rot = s.rot_dim;
+    a.eps = s.eps;
+    const double values = (double)s.tokens * (s.q_heads + s.kv_heads) * s.head_dim;
+    prof::Range r(st, prof::kQkRopeBwd, 17.0 * values, (wq ? 3.0 : 2.0) * esize * values + 4.0 * s.tokens);
+    const bool inter = s.interleaved != 0, norm = wq != nullptr;
+    if (p.blocks > 0) {
+        if (s.dtype == LORY_F32)
+            launch1<float>(a, p.blocks, inter, norm, st);
+        else
+            launch1<__hip_bfloat16>(a, p.blocks, inter, norm, st);
+    }
+    if (norm)
+        hipLaunchKernelGGL(qk_rope_dw_kernel, dim3((2 * s.head_dim + 63) / 64), dim3(1024), 0, st, (const float *)ws, p.blocks,
+                           s.head_dim, dwq, dwk);
+    return launch_status();
+}
+
+}  // namespace lory
