@@ -65,7 +65,9 @@ def turned(x, pos, freq, inter, sign=1.0, magnitude=False):
     a, b = halves(x, rot, inter)
     if magnitude:
         a, b, c, s = a.abs(), b.abs(), c.abs(), s.abs()
-        return join(x.abs(), a * c + b * s, b * c + a * s, rot, inter)
+        # the angle: four roundings of fp64 between the operator and the reference
+        far = 4 * 2.0 ** -53 * t.abs() / ROPE * (a + b)
+        return join(x.abs(), a * c + b * s + far, b * c + a * s + far, rot, inter)
     return join(x, a * c - b * s, b * c + a * s, rot, inter)
 
 
@@ -122,10 +124,8 @@ def test_rope_strides_far_positions_and_in_place():
     yq, _ = lb.lory_qk_rope(q, kt, pos, freq, k_out=yk, wq=wq, wk=wk, eps=EPS)
     rq, sq = rope_ref(q, wq, pos, freq, False)
     rk, sk = rope_ref(k, wk, pos, freq, False)
-    # the angle itself is off by three roundings of fp64: up to 2^31 radians, 2^-22 * 3 / 2 of a turn of the pair
-    far = 3 * 2.0 ** 31 * 2.0 ** -53
-    within("far q", yq, rq, (ROPE + far) * sq, torch.bfloat16)
-    within("far k", yk, rk, (ROPE + far) * sk, torch.bfloat16)
+    within("far q", yq, rq, ROPE * sq, torch.bfloat16)
+    within("far k", yk, rk, ROPE * sk, torch.bfloat16)
     vv = v.clone()
     out = lb.lory_qk_rope(q, k, pos, freq, q_out=q, k_out=k, wq=wq, wk=wk, eps=EPS)
     assert out[0].data_ptr() == q.data_ptr() and torch.equal(q, yq) and torch.equal(k, yk) and torch.equal(v, vv)
@@ -191,7 +191,8 @@ def test_rope_gradient(n, Hq, Hkv, D, rot, inter, dtype):
 
 def test_rope_gradient_against_differences():
     """Central differences of the operator's own forward: the truncation is h^2 / 6 of third derivatives of order 1, the
-    rounding of the two sums of 384 values of order 1 about 384 * 8 * 2^-24 / (2 h); h = 2^-6 makes both below 2e-2."""
+    rounding that of the 64 values that change, of order 2 with their gradient: 64 * 2 * 24 * 2^-24 / (2 h); with
+    h = 2^-6 both stay below 2e-2."""
     g = gen(5)
     n, H, D, rot = 2, 3, 64, 32
     q, k, dy = rnd(g, n, H, D), rnd(g, n, 1, D), rnd(g, n, H, D)
@@ -364,7 +365,7 @@ def test_plan_takes_pages_that_come_back():
 
 @pytest.mark.parametrize("change,status", [(dict(room=-1), 1), (dict(lens0=16 * 4 - 1, add0=2), 2), (dict(count=2), 4),
                                            (dict(count=9, end=True), 8), (dict(lens0=-3), 16), (dict(count=-1), 16 + 4),
-                                           (dict(count=10), 16 + 8), (dict(lens0=65, add0=-1), 16 + 8),
+                                           (dict(count=10), 16 + 8), (dict(lens0=65, add0=-1), 16),
                                            (dict(lens0=2 ** 31 - 1, add0=2 ** 31 - 1), 1 + 2 + 4)])
 def test_plan_status(change, status):
     table = np.array([[0, 1, 2, 3], [4, -1, -1, -1]])
@@ -383,7 +384,7 @@ def test_plan_without_rows():
     one = lambda v: torch.tensor([v], dtype=torch.int32, device="cuda")
     free, cu, cn, st = one(3), one(9), one(9), one(9)
     pos, slots = torch.full((5,), 9, dtype=torch.int32, device="cuda"), torch.full((5,), 9, device="cuda")
-    lb.lory_kv_plan(e, e, e.view(0, 0).new_empty(0, 4), free, one(1), 16, e, cu, pos, slots, cn, st)
+    lb.lory_kv_plan(e, e, torch.empty(0, 4, dtype=torch.int32, device="cuda"), free, one(1), 16, e, cu, pos, slots, cn, st)
     assert cu.item() == 0 and cn.item() == 1 and st.item() == 0 and (pos == 0).all() and (slots == -1).all()
 
 
@@ -450,6 +451,12 @@ def check_attention(label, out, lse, q, k, v, table, lens, scale=None, skip=None
     within(f"{label} lse", lse, rlse, lbound)
 
 
+def same(a, b):
+    """Equal bit for bit, NaN included."""
+    i = torch.int16 if a.dtype == torch.bfloat16 else torch.int32
+    return torch.equal(a.contiguous().view(i), b.contiguous().view(i))
+
+
 def attend(case, **kw):
     q, k, v, table, lens = case
     lse = torch.full(q.shape[:2], 77.0, device="cuda")
@@ -457,8 +464,8 @@ def attend(case, **kw):
     ws.fill_(255)
     out = lb.lory_paged_attn(q, k, v, table, lens, lse=lse, workspace=ws, **kw)
     lse2 = torch.empty_like(lse)
-    assert torch.equal(out, lb.lory_paged_attn(q, k, v, table, lens, lse=lse2, **kw)) and torch.equal(lse, lse2)
-    assert torch.equal(out, lb.lory_paged_attn(q, k, v, table, lens, **kw))   # without lse
+    assert same(out, lb.lory_paged_attn(q, k, v, table, lens, lse=lse2, **kw)) and same(lse, lse2)
+    assert same(out, lb.lory_paged_attn(q, k, v, table, lens, **kw))   # without lse
     return out, lse
 
 
@@ -547,7 +554,6 @@ def test_attention_extreme_scores(dtype):
     within("lowest", out[1, 0], mean, (2.0 ** -16 + 200 * E32) * torch.ones_like(mean), t)
     assert abs(lse[1, 0].item() / (torch.finfo(t).min / 8) - 1) < 8 * E32
     assert torch.isnan(out[3, 1, 7]) and torch.isnan(out).sum() == 1
-    rows = [0, 2, 3]
     keep = [(0, 1), (2, 0), (2, 1), (3, 0)]
     kk, vv = k.clone(), v.clone()
     kk[p0, 0], vv[p3[3], 1, 5, 7] = 0, 0
@@ -555,7 +561,6 @@ def test_attention_extreme_scores(dtype):
     for b, h in keep:
         assert torch.equal(out[b, h], ref_out[b, h]) and lse[b, h] == ref_lse[b, h]
     check_attention("large", ref_out[2:3], ref_lse[2:3], q[2:3], kk, vv, table[2:3], lens[2:3])
-    assert rows
 
 
 def test_attention_cache_above_32_bits():
@@ -616,6 +621,7 @@ def test_on_another_stream_and_in_a_graph():
     eager, side, captured = Step(), Step(), Step()
     stream = torch.cuda.Stream()
     graph = torch.cuda.CUDAGraph()
+    Step().run()
     with torch.cuda.graph(graph):
         captured.run()
     for i in range(25):
