@@ -34,7 +34,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kGroups = 512;   // workgroups: two on each of 256 CUs
+constexpr int kGroups = 512;   // workgroups that share long rows: two on each of 256 CUs
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Args {
@@ -48,9 +48,11 @@ struct Args {
     long out_row, out_head;   // bytes
     float *lse;
     int32_t *starts;          // workspace: units of one head before each row, [rows + 1]
-    float *part_o, *part_ml;  // pieces: [2 * kGroups][16][D] and [2 * kGroups][16][2]
+    float *part_o;            // pieces: [2 * kGroups][16][D]
+    float2 *part_ml;          // [2 * kGroups][16], maximum and sum
     int rows, Hq, Hkv, D, pages, page, width;
     int group, tiles;         // query heads of a key-value head, and blocks of 16 of them
+    int groups;               // workgroups that share the units
     paged::Divider div;       // by page
     float scale2;             // scale * log2(e)
 };
@@ -68,9 +70,6 @@ template <typename T> __device__ __forceinline__ int units_of(int len)
 {
     return len <= kTile<T> ? 1 : (len + kTile<T> - 1) / kTile<T>;   // an empty row has one, which writes its zeros
 }
-
-__device__ __forceinline__ int owner(long u, long U) { return paged::owner(u, U, kGroups); }
-__device__ __forceinline__ long range_begin(int w, long U) { return paged::range_begin(w, U, kGroups); }
 
 __device__ __forceinline__ float xor_max(float v)
 {
@@ -266,35 +265,157 @@ template <int DP, bool PAD> struct Wave<float, DP, PAD> {
     }
 };
 
-template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Args a)
+// LDS of a workgroup of NW wavefronts.
+template <int DP, int NW> struct Shared {
+    float o[NW][16][DP + 4];   // a wavefront's output, unnormalised
+    float m[NW][16], l[NW][16];
+};
+
+// Tiles t0 .. t1 of head h (a block of up to 16 query heads of a key-value head) of row b, whose length is len: the
+// wavefronts take turns of kKeys keys and join in LDS.  `whole`: the piece is all of the row, its result goes to out; else
+// it goes to slot `slot` of the workspace.
+template <typename T, int DP, bool PAD, int NW>
+__device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, int h, int t0, int t1, int len, bool whole, int slot)
 {
     using W = Wave<T, DP, PAD>;
-    constexpr int KEYS = kKeys<T>, TILE = kTile<T>, NS = KEYS / 4;
-    constexpr int LD = DP + 4;   // row of the LDS copy of a wavefront's output
-    __shared__ float so[kWaves][16][LD];
-    __shared__ float sm[kWaves][16], sl[kWaves][16];
-    __shared__ int sums[kThreads + 1], wsum[kWaves];
+    constexpr int KEYS = kKeys<T>, STEP = KEYS * NW, NS = KEYS / 4;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, c = lane >> 4;
+    const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;   // first query head
+    const int nq = min(16, (kvh + 1) * a.group - first);
+    const int last = min(t1 * kTile<T>, len);
+
+    W w;
+    // page of the lane's key of the step at `at`, -1 where there is none
+    const int32_t *pages = a.table + b * a.table_row;
+    auto page_of = [&](int at) {
+        const int t = at + (lane & (KEYS - 1));
+        return t < last ? pages[paged::quotient(a.div, t)] : -1;
+    };
+    auto row_of = [&](int at, int page) {
+        return paged::cache_row(a.div, at + (lane & (KEYS - 1)), page, a.pages, a.Hkv, kvh);
+    };
+    int at = t0 * kTile<T> + wave * KEYS;
+    int page = page_of(at), next = page_of(at + STEP);
+    w.load_q(a.q + b * a.q_row + (first + i) * a.q_head, a.D, c, i < nq);
+#pragma unroll
+    for (int t = 0; t < W::NT; ++t) w.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+
+    int row = row_of(at, page);
+    if (at < last) {
+        w.load_k(a.k, max(row, 0), a.D, i, c);
+        w.load_v(a.v, max(row, 0), a.D, i, c);
+    }
+    for (; at < last; at += STEP) {
+        const uint32_t valid = (uint32_t)__ballot(row >= 0);
+        const int row1 = row_of(at + STEP, next);
+        next = page_of(at + 2 * STEP);
+        const bool more = at + STEP < last;
+
+        float s[NS];
+        w.scores(s);
+        if (more) w.load_k(a.k, max(row1, 0), a.D, i, c);
+
+        float top = -INFINITY;
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            s[n] = (valid >> ((n >> 2) * 16 + 4 * c + (n & 3))) & 1 ? s[n] * a.scale2 : -INFINITY;
+            top = fmaxf(top, s[n]);
+        }
+        const float m1 = fmaxf(m, xor_max(top));
+        const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing but -inf so far: every weight is 0
+        if (__any(m1 != m)) {
+            const float f = __builtin_amdgcn_exp2f(m - ref);
+            l *= f;
+#pragma unroll
+            for (int t = 0; t < W::NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) w.o[t][r] *= f;
+        }
+        m = m1;
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            s[n] = __builtin_amdgcn_exp2f(s[n] - ref);
+            l += s[n];
+        }
+        if (valid != (uint32_t)((1ull << KEYS) - 1)) w.clear_v(valid, c);
+        w.add(s);
+        if (more) w.load_v(a.v, max(row1, 0), a.D, i, c);
+        row = row1;
+    }
+    l = xor_sum(l);
+
+    if (c == 0) {
+        sh.m[wave][i] = m;
+        sh.l[wave][i] = l;
+    }
+    if (i < nq) {
+#pragma unroll
+        for (int t = 0; t < W::NT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sh.o[wave][i][W::dim(t, 4 * c + r)] = w.o[t][r];
+    }
+    __syncthreads();
+    for (int x = tid; x < nq * a.D; x += 64 * NW) {
+        const int j = x / a.D, d = x - j * a.D;
+        float M = sh.m[0][j];
+#pragma unroll
+        for (int n = 1; n < NW; ++n) M = fmaxf(M, sh.m[n][j]);
+        const float ref = M == -INFINITY ? 0.f : M;
+        float L = 0.f, O = 0.f;
+#pragma unroll
+        for (int n = 0; n < NW; ++n) {
+            const float f = __builtin_amdgcn_exp2f(sh.m[n][j] - ref);
+            L = fmaf(f, sh.l[n][j], L);
+            O = fmaf(f, sh.o[n][j][d], O);
+        }
+        if (whole) {
+            Elem<T>::store((T *)(a.out + b * a.out_row + (first + j) * a.out_head) + d, O / (L == 0.f ? 1.f : L));
+            if (d == 0 && a.lse) a.lse[(long)b * a.Hq + first + j] = (ref + log2f(L)) * kLn2;
+        } else {
+            a.part_o[((long)slot * 16 + j) * a.D + d] = O;
+            if (d == 0) a.part_ml[slot * 16 + j] = make_float2(M, L);
+        }
+    }
+    __syncthreads();
+}
+
+// Short rows: a workgroup takes all of a row's head, and nothing is left to join.
+template <typename T, int DP, bool PAD, int NW> __global__ __launch_bounds__(64 * NW) void paged_attn_rows_kernel(Args a)
+{
+    __shared__ Shared<DP, NW> sh;
+    const int heads = a.Hkv * a.tiles;
+    for (long item = blockIdx.x; item < (long)a.rows * heads; item += gridDim.x) {
+        const int b = (int)(item / heads), h = (int)(item - (long)b * heads);
+        const int len = length_of(a, b);
+        piece<T, DP, PAD, NW>(a, sh, b, h, 0, units_of<T>(len), len, true, 0);
+    }
+}
+
+// Long rows: equal ranges of the units of all rows and heads.
+template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Args a)
+{
+    __shared__ Shared<DP, kWaves> sh;
+    __shared__ int sums[kThreads + 1], wsum[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int heads = a.Hkv * a.tiles;
 
     // units of one head before each chunk of rows
     const int chunk = (a.rows + kThreads - 1) / kThreads;
-    {
-        int n = 0;
-        for (int b = tid * chunk; b < min((tid + 1) * chunk, a.rows); ++b) n += units_of<T>(length_of(a, b));
-        for (int m = 1; m < 64; m <<= 1) {
-            const int u = __shfl_up(n, m, 64);
-            if (lane >= m) n += u;
-        }
-        if (lane == 63) wsum[wave] = n;
-        __syncthreads();
-        for (int w = 0; w < wave; ++w) n += wsum[w];
-        sums[tid + 1] = n;
-        if (tid == 0) sums[0] = 0;
-        __syncthreads();
+    int n = 0;
+    for (int b = tid * chunk; b < min((tid + 1) * chunk, a.rows); ++b) n += units_of<T>(length_of(a, b));
+    for (int m = 1; m < 64; m <<= 1) {
+        const int u = __shfl_up(n, m, 64);
+        if (lane >= m) n += u;
     }
+    if (lane == 63) wsum[wave] = n;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) n += wsum[w];
+    sums[tid + 1] = n;
+    if (tid == 0) sums[0] = 0;
+    __syncthreads();
     if (blockIdx.x == 0) {   // for the launch that joins
-        int n = sums[tid];
+        n = sums[tid];
         for (int b = tid * chunk; b < min((tid + 1) * chunk, a.rows); ++b) {
             a.starts[b] = n;
             n += units_of<T>(length_of(a, b));
@@ -302,136 +423,29 @@ template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) v
         if (tid == 0) a.starts[a.rows] = sums[kThreads];
     }
     const long U = (long)sums[kThreads] * heads;
-    long u = range_begin(blockIdx.x, U);
-    const long end = range_begin(blockIdx.x + 1, U);
+    long u = paged::range_begin(blockIdx.x, U, a.groups);
+    const long end = paged::range_begin(blockIdx.x + 1, U, a.groups);
     if (u >= end) return;
 
     // row, head and tile of the first unit
-    int b, h, tile, len, units;
-    {
-        int lo = 0, hi = kThreads;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if ((long)sums[mid] * heads <= u) lo = mid; else hi = mid;
-        }
-        b = lo * chunk;
-        long rest = u - (long)sums[lo] * heads;
-        for (;; ++b) {
-            len = length_of(a, b);
-            units = units_of<T>(len);
-            if (rest < (long)units * heads || b == a.rows - 1) break;
-            rest -= (long)units * heads;
-        }
-        h = (int)(rest / units);
-        tile = (int)(rest - (long)h * units);
+    int lo = 0, hi = kThreads;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((long)sums[mid] * heads <= u) lo = mid; else hi = mid;
     }
+    int b = lo * chunk, len, units;
+    long rest = u - (long)sums[lo] * heads;
+    for (;; ++b) {
+        len = length_of(a, b);
+        units = units_of<T>(len);
+        if (rest < (long)units * heads || b == a.rows - 1) break;
+        rest -= (long)units * heads;
+    }
+    int h = (int)(rest / units), tile = (int)(rest - (long)h * units);
 
-    W w;
     while (u < end) {
         const int stop = (int)(end - u < units - tile ? tile + (end - u) : units);
-        const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;   // first query head
-        const int nq = min(16, (kvh + 1) * a.group - first);
-        const int last = min(stop * TILE, len);
-
-        w.load_q(a.q + b * a.q_row + (first + i) * a.q_head, a.D, c, i < nq);
-#pragma unroll
-        for (int t = 0; t < W::NT; ++t) w.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float m = -INFINITY, l = 0.f;
-
-        // page of the lane's key of the step at `at`, -1 where there is none
-        const int32_t *pages = a.table + b * a.table_row;
-        auto page_of = [&](int at) {
-            const int t = at + (lane & (KEYS - 1));
-            return t < last ? pages[paged::quotient(a.div, t)] : -1;
-        };
-        auto row_of = [&](int at, int page) {
-            return paged::cache_row(a.div, at + (lane & (KEYS - 1)), page, a.pages, a.Hkv, kvh);
-        };
-        int at = tile * TILE + wave * KEYS;
-        int row = row_of(at, page_of(at)), next = page_of(at + TILE);
-        if (at < last) {
-            w.load_k(a.k, max(row, 0), a.D, i, c);
-            w.load_v(a.v, max(row, 0), a.D, i, c);
-        }
-        for (; at < last; at += TILE) {
-            const uint32_t valid = (uint32_t)__ballot(row >= 0);
-            const int row1 = row_of(at + TILE, next);
-            next = page_of(at + 2 * TILE);
-            const bool more = at + TILE < last;
-
-            float s[NS];
-            w.scores(s);
-            if (more) w.load_k(a.k, max(row1, 0), a.D, i, c);
-
-            float top = -INFINITY;
-#pragma unroll
-            for (int n = 0; n < NS; ++n) {
-                s[n] = (valid >> ((n >> 2) * 16 + 4 * c + (n & 3))) & 1 ? s[n] * a.scale2 : -INFINITY;
-                top = fmaxf(top, s[n]);
-            }
-            const float m1 = fmaxf(m, xor_max(top));
-            const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing but -inf so far: every weight is 0
-            if (__any(m1 != m)) {
-                const float f = exp2f(m - ref);
-                l *= f;
-#pragma unroll
-                for (int t = 0; t < W::NT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) w.o[t][r] *= f;
-            }
-            m = m1;
-#pragma unroll
-            for (int n = 0; n < NS; ++n) {
-                s[n] = exp2f(s[n] - ref);
-                l += s[n];
-            }
-            if (valid != (uint32_t)((1ull << KEYS) - 1)) w.clear_v(valid, c);
-            w.add(s);
-            if (more) w.load_v(a.v, max(row1, 0), a.D, i, c);
-            row = row1;
-        }
-        l = xor_sum(l);
-
-        // the four wavefronts together
-        if (c == 0) {
-            sm[wave][i] = m;
-            sl[wave][i] = l;
-        }
-        if (i < nq) {
-#pragma unroll
-            for (int t = 0; t < W::NT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) so[wave][i][W::dim(t, 4 * c + r)] = w.o[t][r];
-        }
-        __syncthreads();
-        const bool whole = tile == 0 && stop == units;
-        const int slot = 2 * blockIdx.x + (tile == 0 ? 1 : 0);
-        for (int x = tid; x < nq * a.D; x += kThreads) {
-            const int j = x / a.D, d = x - j * a.D;
-            float M = sm[0][j];
-#pragma unroll
-            for (int n = 1; n < kWaves; ++n) M = fmaxf(M, sm[n][j]);
-            const float ref = M == -INFINITY ? 0.f : M;
-            float L = 0.f, O = 0.f;
-#pragma unroll
-            for (int n = 0; n < kWaves; ++n) {
-                const float f = exp2f(sm[n][j] - ref);
-                L = fmaf(f, sl[n][j], L);
-                O = fmaf(f, so[n][j][d], O);
-            }
-            if (whole) {
-                Elem<T>::store((T *)(a.out + b * a.out_row + (first + j) * a.out_head) + d, O / (L == 0.f ? 1.f : L));
-                if (d == 0 && a.lse) a.lse[(long)b * a.Hq + first + j] = (ref + log2f(L)) * kLn2;
-            } else {
-                a.part_o[((long)slot * 16 + j) * a.D + d] = O;
-                if (d == 0) {
-                    a.part_ml[(slot * 16 + j) * 2] = M;
-                    a.part_ml[(slot * 16 + j) * 2 + 1] = L;
-                }
-            }
-        }
-        __syncthreads();
-
+        piece<T, DP, PAD, kWaves>(a, sh, b, h, tile, stop, len, tile == 0 && stop == units, 2 * blockIdx.x + (tile == 0 ? 1 : 0));
         u += stop - tile;
         tile = 0;
         if (stop == units && ++h == heads && u < end) {
@@ -443,44 +457,116 @@ template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) v
     }
 }
 
-// Joins the pieces of one row's head: grid (heads, rows).
+// Joins the pieces of one row's head, grid (heads, rows).  16 threads a query find the maximum and the sum; then every thread
+// adds four dims of one query over a share of the pieces, and the shares are added in order.
 template <typename T> __global__ __launch_bounds__(kThreads) void paged_attn_join_kernel(Args a)
 {
-    const int h = blockIdx.x, heads = gridDim.x;
+    __shared__ float sm[16], sl[16];
+    __shared__ f32x4 so[kThreads];
+    const int h = blockIdx.x, heads = gridDim.x, tid = threadIdx.x;
     for (int b = blockIdx.y; b < a.rows; b += gridDim.y) {
         const long U = (long)a.starts[a.rows] * heads;
         const int units = a.starts[b + 1] - a.starts[b];
-        const long u0 = (long)a.starts[b] * heads + (long)h * units, u1 = u0 + units;
-        const int w0 = owner(u0, U), w1 = owner(u1 - 1, U);
+        const long u0 = (long)a.starts[b] * heads + (long)h * units;
+        const int w0 = paged::owner(u0, U, a.groups), w1 = paged::owner(u0 + units - 1, U, a.groups);
         if (w0 == w1) continue;   // written already
+        // pieces lie with consecutive workgroups, or with those that have a unit at all
+        const bool dense = U >= a.groups;
+        const int parts = dense ? w1 - w0 + 1 : units;
+        auto slot_of = [&](int p) { return p == 0 ? 2 * w0 + 1 : 2 * (dense ? w0 + p : paged::owner(u0 + p, U, a.groups)); };
         const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;
         const int nq = min(16, (kvh + 1) * a.group - first);
-        for (int x = threadIdx.x; x < nq * a.D; x += kThreads) {
-            const int j = x / a.D, d = x - j * a.D;
-            float M = -INFINITY, L = 0.f, O = 0.f;
-            for (int w = w0; w <= w1; ++w) {
-                if (range_begin(w, U) == range_begin(w + 1, U)) continue;
-                const int slot = 2 * w + (w == w0 ? 1 : 0);
-                const float m = a.part_ml[(slot * 16 + j) * 2], l = a.part_ml[(slot * 16 + j) * 2 + 1];
-                const float M1 = fmaxf(M, m), ref = M1 == -INFINITY ? 0.f : M1;
-                const float f = exp2f(M - ref), g = exp2f(m - ref);
-                L = L * f + l * g;
-                O = O * f + a.part_o[((long)slot * 16 + j) * a.D + d] * g;
-                M = M1;
+
+        const int j = tid >> 4, k = tid & 15;
+        float M = -INFINITY, L = 0.f;
+        if (j < nq)
+            for (int p = k; p < parts; p += 16) M = fmaxf(M, a.part_ml[slot_of(p) * 16 + j].x);
+#pragma unroll
+        for (int m = 1; m < 16; m <<= 1) M = fmaxf(M, __shfl_xor(M, m, 64));
+        const float ref = M == -INFINITY ? 0.f : M;
+        if (j < nq)
+            for (int p = k; p < parts; p += 16) {
+                const float2 ml = a.part_ml[slot_of(p) * 16 + j];
+                L = fmaf(__builtin_amdgcn_exp2f(ml.x - ref), ml.y, L);
             }
-            Elem<T>::store((T *)(a.out + b * a.out_row + (first + j) * a.out_head) + d, O / (L == 0.f ? 1.f : L));
-            if (d == 0 && a.lse) a.lse[(long)b * a.Hq + first + j] = ((M == -INFINITY ? 0.f : M) + log2f(L)) * kLn2;
+#pragma unroll
+        for (int m = 1; m < 16; m <<= 1) L += __shfl_xor(L, m, 64);
+        __syncthreads();   // the row before is done with the sums
+        if (j < nq && k == 0) {
+            sm[j] = ref;
+            sl[j] = L;
+            if (a.lse) a.lse[(long)b * a.Hq + first + j] = (ref + log2f(L)) * kLn2;
+        }
+        __syncthreads();
+
+        const int quads = a.D / 4, all = nq * quads;   // of all queries
+        int per = 16;                                  // threads that share a piece
+        while (per < all && per < kThreads) per <<= 1;
+        const int shares = kThreads / per, share = tid / per;
+        for (int x0 = 0; x0 < all; x0 += per) {
+            const int x = x0 + tid % per;
+            const bool on = x < all;
+            const int jj = on ? x / quads : 0, d = on ? (x - jj * quads) * 4 : 0;
+            const float mref = sm[jj];
+            f32x4 O = {0.f, 0.f, 0.f, 0.f};
+            if (on) {
+#pragma unroll 4
+                for (int p = share; p < parts; p += shares) {
+                    const long slot = (long)slot_of(p) * 16 + jj;
+                    const float f = __builtin_amdgcn_exp2f(a.part_ml[slot].x - mref);
+                    const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part_o + slot * a.D + d);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) O[e] = fmaf(f, v[e], O[e]);
+                }
+            }
+            if (shares > 1) {
+                so[tid] = O;
+                __syncthreads();
+                if (share == 0)
+                    for (int n = 1; n < shares; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) O[e] += so[n * per + tid][e];
+                __syncthreads();
+            }
+            if (share == 0 && on) {
+                const float LL = sl[jj];
+                T *dst = (T *)(a.out + b * a.out_row + (first + jj) * a.out_head) + d;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) Elem<T>::store(dst + e, O[e] / (LL == 0.f ? 1.f : LL));
+            }
         }
     }
+}
+
+// Rows up to this many tokens (of the table, the lengths are on the device) take no second launch.
+template <typename T> constexpr int kShortRow = 8 * kTile<T>;
+
+template <typename T, int DP, bool PAD> void launch3(const Args &a, hipStream_t st)
+{
+    const long items = (long)a.rows * a.Hkv * a.tiles;
+    if ((long)a.width * a.page <= kShortRow<T>) {
+        const dim3 grid((unsigned)(items < 65536 ? items : 65536));
+        if constexpr (DP <= 128) {   // eight wavefronts of the widest heads would spill
+            if (items <= 256) {
+                hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 8>), grid, dim3(512), 0, st, a);
+                return;
+            }
+        }
+        hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 4>), grid, dim3(256), 0, st, a);
+        return;
+    }
+    Args g = a;
+    g.groups = DP == 256 ? kGroups / 2 : kGroups;   // what the registers let run at a time
+    hipLaunchKernelGGL((paged_attn_kernel<T, DP, PAD>), dim3(g.groups), dim3(kThreads), 0, st, g);
+    hipLaunchKernelGGL((paged_attn_join_kernel<T>), dim3(a.Hkv * a.tiles, a.rows < 32768 ? a.rows : 32768), dim3(kThreads), 0, st, g);
 }
 
 template <typename T, int DP> void launch2(const Args &a, hipStream_t st)
 {
     if (a.D == DP)
-        hipLaunchKernelGGL((paged_attn_kernel<T, DP, false>), dim3(kGroups), dim3(kThreads), 0, st, a);
+        launch3<T, DP, false>(a, st);
     else
-        hipLaunchKernelGGL((paged_attn_kernel<T, DP, true>), dim3(kGroups), dim3(kThreads), 0, st, a);
-    hipLaunchKernelGGL((paged_attn_join_kernel<T>), dim3(a.Hkv * a.tiles, a.rows < 32768 ? a.rows : 32768), dim3(kThreads), 0, st, a);
+        launch3<T, DP, true>(a, st);
 }
 
 template <typename T> void launch1(const Args &a, hipStream_t st)
@@ -521,7 +607,7 @@ int paged_attn_launch(const lory_paged_shape &s, const lory_heads &q, const void
     a.lse = lse;
     a.starts = (int32_t *)ws;
     a.part_o = (float *)((char *)ws + starts_bytes(s));
-    a.part_ml = a.part_o + (size_t)2 * kGroups * 16 * s.head_dim;
+    a.part_ml = (float2 *)(a.part_o + (size_t)2 * kGroups * 16 * s.head_dim);
     a.rows = s.rows;
     a.Hq = s.q_heads;
     a.Hkv = s.kv_heads;
