@@ -34,7 +34,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kGroups = 512;   // workgroups that share long rows: two on each of 256 CUs
+constexpr int kGroups = 512;   // workgroups that fill the chip: two on each of 256 CUs
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Args {
@@ -48,11 +48,12 @@ struct Args {
     long out_row, out_head;   // bytes
     float *lse;
     int32_t *starts;          // workspace: units of one head before each row, [rows + 1]
-    float *part_o;            // pieces: [2 * kGroups][16][D]
-    float2 *part_ml;          // [2 * kGroups][16], maximum and sum
+    float *part_o;            // pieces: [slots][part_rows][D]
+    float2 *part_ml;          // [slots][part_rows], maximum and sum
+    int part_rows;
     int rows, Hq, Hkv, D, pages, page, width;
     int group, tiles;         // query heads of a key-value head, and blocks of 16 of them
-    int groups;               // workgroups that share the units
+    int groups;               // ranges that share the units
     paged::Divider div;       // by page
     float scale2;             // scale * log2(e)
 };
@@ -373,26 +374,29 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             Elem<T>::store((T *)(a.out + b * a.out_row + (first + j) * a.out_head) + d, O / (L == 0.f ? 1.f : L));
             if (d == 0 && a.lse) a.lse[(long)b * a.Hq + first + j] = (ref + log2f(L)) * kLn2;
         } else {
-            a.part_o[((long)slot * 16 + j) * a.D + d] = O;
-            if (d == 0) a.part_ml[slot * 16 + j] = make_float2(M, L);
+            a.part_o[((long)slot * a.part_rows + j) * a.D + d] = O;
+            if (d == 0) a.part_ml[(long)slot * a.part_rows + j] = make_float2(M, L);
         }
     }
     __syncthreads();
 }
 
-// Short rows: a workgroup takes all of a row's head, and nothing is left to join.
+// A row's units in a.groups equal ranges, a workgroup each (one range: all of the row, and nothing is left to join).
 template <typename T, int DP, bool PAD, int NW> __global__ __launch_bounds__(64 * NW) void paged_attn_rows_kernel(Args a)
 {
     __shared__ Shared<DP, NW> sh;
-    const int heads = a.Hkv * a.tiles;
-    for (long item = blockIdx.x; item < (long)a.rows * heads; item += gridDim.x) {
-        const int b = (int)(item / heads), h = (int)(item - (long)b * heads);
-        const int len = length_of(a, b);
-        piece<T, DP, PAD, NW>(a, sh, b, h, 0, units_of<T>(len), len, true, 0);
+    const int heads = a.Hkv * a.tiles, S = a.groups;
+    const long all = (long)a.rows * heads * S;
+    for (long x = blockIdx.x; x < all; x += gridDim.x) {
+        const long item = x / S;
+        const int s = (int)(x - item * S), b = (int)(item / heads), h = (int)(item - (long)b * heads);
+        const int len = length_of(a, b), units = units_of<T>(len);
+        const int t0 = (int)paged::range_begin(s, units, S), t1 = (int)paged::range_begin(s + 1, units, S);
+        if (t0 < t1) piece<T, DP, PAD, NW>(a, sh, b, h, t0, t1, len, t0 == 0 && t1 == units, (int)x);
     }
 }
 
-// Long rows: equal ranges of the units of all rows and heads.
+// Equal ranges of the units of all rows and heads.
 template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Args a)
 {
     __shared__ Shared<DP, kWaves> sh;
@@ -458,35 +462,39 @@ template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) v
 }
 
 // Joins the pieces of one row's head, grid (heads, rows).  16 threads a query find the maximum and the sum; then every thread
-// adds four dims of one query over a share of the pieces, and the shares are added in order.
-template <typename T> __global__ __launch_bounds__(kThreads) void paged_attn_join_kernel(Args a)
+// adds four dims of one query over a share of the pieces, and the shares are added in order.  BY_ROW: the pieces are those of
+// paged_attn_rows_kernel.
+template <typename T, bool BY_ROW> __global__ __launch_bounds__(kThreads) void paged_attn_join_kernel(Args a)
 {
     __shared__ float sm[16], sl[16];
     __shared__ f32x4 so[kThreads];
     const int h = blockIdx.x, heads = gridDim.x, tid = threadIdx.x;
     for (int b = blockIdx.y; b < a.rows; b += gridDim.y) {
-        const long U = (long)a.starts[a.rows] * heads;
-        const int units = a.starts[b + 1] - a.starts[b];
-        const long u0 = (long)a.starts[b] * heads + (long)h * units;
+        const int units = BY_ROW ? units_of<T>(length_of(a, b)) : a.starts[b + 1] - a.starts[b];
+        const long U = BY_ROW ? units : (long)a.starts[a.rows] * heads;
+        const long u0 = BY_ROW ? 0 : (long)a.starts[b] * heads + (long)h * units;
         const int w0 = paged::owner(u0, U, a.groups), w1 = paged::owner(u0 + units - 1, U, a.groups);
         if (w0 == w1) continue;   // written already
-        // pieces lie with consecutive workgroups, or with those that have a unit at all
+        // pieces lie with consecutive ranges, or with those that have a unit at all
         const bool dense = U >= a.groups;
         const int parts = dense ? w1 - w0 + 1 : units;
-        auto slot_of = [&](int p) { return p == 0 ? 2 * w0 + 1 : 2 * (dense ? w0 + p : paged::owner(u0 + p, U, a.groups)); };
+        auto slot_of = [&](int p) {
+            const int w = dense ? w0 + p : paged::owner(u0 + p, U, a.groups);
+            return BY_ROW ? (b * heads + h) * a.groups + w : 2 * w + (p == 0);
+        };
         const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;
         const int nq = min(16, (kvh + 1) * a.group - first);
 
         const int j = tid >> 4, k = tid & 15;
         float M = -INFINITY, L = 0.f;
         if (j < nq)
-            for (int p = k; p < parts; p += 16) M = fmaxf(M, a.part_ml[slot_of(p) * 16 + j].x);
+            for (int p = k; p < parts; p += 16) M = fmaxf(M, a.part_ml[(long)slot_of(p) * a.part_rows + j].x);
 #pragma unroll
         for (int m = 1; m < 16; m <<= 1) M = fmaxf(M, __shfl_xor(M, m, 64));
         const float ref = M == -INFINITY ? 0.f : M;
         if (j < nq)
             for (int p = k; p < parts; p += 16) {
-                const float2 ml = a.part_ml[slot_of(p) * 16 + j];
+                const float2 ml = a.part_ml[(long)slot_of(p) * a.part_rows + j];
                 L = fmaf(__builtin_amdgcn_exp2f(ml.x - ref), ml.y, L);
             }
 #pragma unroll
@@ -512,7 +520,7 @@ template <typename T> __global__ __launch_bounds__(kThreads) void paged_attn_joi
             if (on) {
 #pragma unroll 4
                 for (int p = share; p < parts; p += shares) {
-                    const long slot = (long)slot_of(p) * 16 + jj;
+                    const long slot = (long)slot_of(p) * a.part_rows + jj;
                     const float f = __builtin_amdgcn_exp2f(a.part_ml[slot].x - mref);
                     const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part_o + slot * a.D + d);
 #pragma unroll
@@ -538,54 +546,91 @@ template <typename T> __global__ __launch_bounds__(kThreads) void paged_attn_joi
     }
 }
 
-// Rows up to this many tokens (of the table, the lengths are on the device) take no second launch.
-template <typename T> constexpr int kShortRow = 8 * kTile<T>;
+struct Plan {
+    int ranges;    // of every row, 0: ranges over all rows
+    int slots;     // pieces that the workspace has room for
+};
 
-template <typename T, int DP, bool PAD> void launch3(const Args &a, hipStream_t st)
+// How the units are cut, from the longest rows that the table allows (the lengths are on the device).  One workgroup takes
+// in about 60 bytes per ns, the second launch and the pieces cost 5 us:
+//  - a workgroup per row and head where that is at most 256 KB of keys and values, or up to 1 MB with so many rows that they
+//    fill the chip (us, one launch / cut; bf16, heads of 128: 2 heads of 512 tokens 8.8 / 9.1, of 1024 12.6 / 9.1; 64 of
+//    1024 14.5 / 14.1; 160 of 1024 17.1 / 23.2; 200 of 2048 41 / 50, of 4096 78 / 86);
+//  - every row cut alike where the ranges fill the chip once at most and the longest is short, so that it does not matter whose
+//    row is long (28 heads of up to 3001 tokens, fp32: 18.1 us, 20.4 with ranges over all rows; with longer ranges a
+//    ragged batch of 48 rows takes 46 us against 31);
+//  - else equal ranges over all rows, which costs the sums over their lengths.
+Plan plan(const lory_paged_shape &s)
 {
-    const long items = (long)a.rows * a.Hkv * a.tiles;
-    if ((long)a.width * a.page <= kShortRow<T>) {
-        const dim3 grid((unsigned)(items < 65536 ? items : 65536));
+    const int esize = s.dtype == LORY_F32 ? 4 : 2, tile = s.dtype == LORY_F32 ? kTile<float> : kTile<__hip_bfloat16>;
+    const int group = s.q_heads / s.kv_heads;
+    const long items = (long)s.rows * s.kv_heads * ((group + 15) / 16), most = ((long)s.width * s.page + tile - 1) / tile;
+    const long row_bytes = 2 * most * tile * s.head_dim * esize, KB = 1024;
+    if (most == 1 || row_bytes <= 256 * KB || row_bytes <= (items < 128 ? items * 8 * KB : 1024 * KB)) return {1, 0};
+    const long n = items > 0 ? (kGroups / items < most ? kGroups / items : most) : 1;
+    if (n > 1 && row_bytes <= n * 256 * KB) return {(int)n, (int)(n * items)};
+    return {0, 2 * kGroups};
+}
+
+template <typename T, int DP, bool PAD> void launch3(const Args &a, const Plan &p, hipStream_t st)
+{
+    const dim3 join(a.Hkv * a.tiles, a.rows < 32768 ? a.rows : 32768);
+    Args g = a;
+    if (p.ranges) {
+        g.groups = p.ranges;
+        const long all = (long)a.rows * a.Hkv * a.tiles * p.ranges;
+        const dim3 grid((unsigned)(all < 65536 ? all : 65536));
+        bool wide = false;
         if constexpr (DP <= 128) {   // eight wavefronts of the widest heads would spill
-            if (items <= 256) {
-                hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 8>), grid, dim3(512), 0, st, a);
-                return;
-            }
+            wide = all <= 256;
+            if (wide) hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 8>), grid, dim3(512), 0, st, g);
         }
-        hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 4>), grid, dim3(256), 0, st, a);
+        if (!wide) hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 4>), grid, dim3(256), 0, st, g);
+        if (p.ranges > 1) hipLaunchKernelGGL((paged_attn_join_kernel<T, true>), join, dim3(kThreads), 0, st, g);
         return;
     }
-    Args g = a;
     g.groups = DP == 256 ? kGroups / 2 : kGroups;   // what the registers let run at a time
     hipLaunchKernelGGL((paged_attn_kernel<T, DP, PAD>), dim3(g.groups), dim3(kThreads), 0, st, g);
-    hipLaunchKernelGGL((paged_attn_join_kernel<T>), dim3(a.Hkv * a.tiles, a.rows < 32768 ? a.rows : 32768), dim3(kThreads), 0, st, g);
+    hipLaunchKernelGGL((paged_attn_join_kernel<T, false>), join, dim3(kThreads), 0, st, g);
 }
 
-template <typename T, int DP> void launch2(const Args &a, hipStream_t st)
+template <typename T, int DP> void launch2(const Args &a, const Plan &p, hipStream_t st)
 {
     if (a.D == DP)
-        launch3<T, DP, false>(a, st);
+        launch3<T, DP, false>(a, p, st);
     else
-        launch3<T, DP, true>(a, st);
+        launch3<T, DP, true>(a, p, st);
 }
 
-template <typename T> void launch1(const Args &a, hipStream_t st)
+template <typename T> void launch1(const Args &a, const Plan &p, hipStream_t st)
 {
     if (a.D <= 64)
-        launch2<T, 64>(a, st);
+        launch2<T, 64>(a, p, st);
     else if (a.D <= 128)
-        launch2<T, 128>(a, st);
+        launch2<T, 128>(a, p, st);
     else
-        launch2<T, 256>(a, st);
+        launch2<T, 256>(a, p, st);
 }
 
-size_t starts_bytes(const lory_paged_shape &s) { return align_up(((size_t)s.rows + 1) * sizeof(int32_t), 256); }
+size_t starts_bytes(const lory_paged_shape &s, const Plan &p)
+{
+    return p.ranges ? 0 : align_up(((size_t)s.rows + 1) * sizeof(int32_t), 256);
+}
+
+// queries of a piece
+int part_rows(const lory_paged_shape &s)
+{
+    const int group = s.q_heads / s.kv_heads;
+    return group < 16 ? group : 16;
+}
 
 }  // namespace
 
 size_t paged_attn_workspace_bytes(const lory_paged_shape &s)
 {
-    return align_up(starts_bytes(s) + (size_t)2 * kGroups * 16 * (s.head_dim + 2) * sizeof(float), 256);
+    const Plan p = plan(s);
+    const size_t n = starts_bytes(s, p) + (size_t)p.slots * part_rows(s) * (s.head_dim + 2) * sizeof(float);
+    return align_up(n > 0 ? n : 1, 256);
 }
 
 int paged_attn_launch(const lory_paged_shape &s, const lory_heads &q, const void *k_cache, const void *v_cache,
@@ -605,9 +650,11 @@ int paged_attn_launch(const lory_paged_shape &s, const lory_heads &q, const void
     a.out_row = out.token * esize;
     a.out_head = out.head * esize;
     a.lse = lse;
+    const Plan p = plan(s);
     a.starts = (int32_t *)ws;
-    a.part_o = (float *)((char *)ws + starts_bytes(s));
-    a.part_ml = (float2 *)(a.part_o + (size_t)2 * kGroups * 16 * s.head_dim);
+    a.part_rows = part_rows(s);
+    a.part_o = (float *)((char *)ws + starts_bytes(s, p));
+    a.part_ml = (float2 *)(a.part_o + (size_t)p.slots * a.part_rows * s.head_dim);
     a.rows = s.rows;
     a.Hq = s.q_heads;
     a.Hkv = s.kv_heads;
@@ -621,9 +668,9 @@ int paged_attn_launch(const lory_paged_shape &s, const lory_heads &q, const void
     a.scale2 = s.scale * kLog2e;
     prof::Range r(st, prof::kPagedAttn, 0.0, 0.0);   // the lengths are on the device
     if (s.dtype == LORY_F32)
-        launch1<float>(a, st);
+        launch1<float>(a, p, st);
     else
-        launch1<__hip_bfloat16>(a, st);
+        launch1<__hip_bfloat16>(a, p, st);
     return launch_status();
 }
 
