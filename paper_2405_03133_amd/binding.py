@@ -1,4 +1,5 @@
-"""Thin ctypes binding of liblory.so (C ABI: include/lory.h).
+"""Thin binding of liblory.so (C ABI: include/lory.h): ctypes for the layer, and for the attention operators, whose calls
+are short and have many tensors, the extension module _marshal (csrc/marshal.cpp), which does the same checks.
 
 Argument marshalling only: every function takes torch tensors that already
 live on the GPU, checks dtype / shape / contiguity on the host, and passes raw
@@ -391,55 +392,22 @@ def lory_merged_ffn_bwd(X: torch.Tensor, w: torch.Tensor, Wg: torch.Tensor, Wu: 
 # ---- the attention half: strided heads, a paged key-value cache
 
 
-def _heads(t: torch.Tensor, dtype: torch.dtype, shape: Tuple[int, int, int], name: str) -> LoryHeads:
-    """A [tokens, heads, head_dim] tensor as it lies; only its last index has to be contiguous."""
-    token, head, last = t.stride() if t.dim() == 3 else (0, 0, 1)
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {list(shape)}")
-    if last != 1:
-        raise ValueError(f"the last dimension of {name} must be contiguous")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live on the GPU")
-    return LoryHeads(t.data_ptr(), token, head)
+_native_module = None
 
 
-def _array(t: torch.Tensor, dtype: torch.dtype, n: int, name: str) -> int:
-    """Address of a contiguous array of n elements."""
-    if t.dtype is not dtype or t.shape != (n,):
-        raise ValueError(f"{name} must be {dtype} [{n}]")
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must live on the GPU, contiguous")
-    return t.data_ptr()
-
-
-def _table(t: torch.Tensor, rows: int) -> Tuple[int, int, int]:
-    """Address, width and elements from row to row of a page table."""
-    if t.dtype is not torch.int32 or t.dim() != 2 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"table must be int32 [{rows}, width] with contiguous rows")
-    if not t.is_cuda:
-        raise ValueError("table must live on the GPU")
-    width = t.shape[1]
-    return t.data_ptr(), width, t.stride(0) if rows > 1 else width
+def _native():
+    """The extension module that checks and passes the arguments of the calls below; raise if it has not been built."""
+    global _native_module
+    if _native_module is None:
+        lib()
+        from . import _marshal
+        _native_module = _marshal
+    return _native_module
 
 
 def _rope_shape(q: torch.Tensor, k: torch.Tensor, rot: int, eps: float, interleaved: bool) -> LoryRopeShape:
     n, Hq, D = q.shape
     return LoryRopeShape(n, Hq, k.shape[1], D, rot, interleaved, _dtype_code(q.dtype), eps)
-
-
-def _rope_args(q, k, pos, freq, wq, wk):
-    """Addresses of what the three calls share, after the shapes and type that the other tensors are held against."""
-    n, Hq, D = qs = q.shape
-    ks = (n, k.shape[1], D)
-    dtype = q.dtype
-    for name, t in (("wq", wq), ("wk", wk)):
-        if t is not None and t.dtype is not dtype:
-            raise TypeError(f"{name} must be {dtype}")
-    return (qs, ks, dtype, _heads(q, dtype, qs, "q"), _heads(k, dtype, ks, "k"), _array(pos, torch.int32, n, "pos"),
-            _array(freq, torch.float64, freq.shape[0], "freq"), None if wq is None else _array(wq, dtype, D, "wq"),
-            None if wk is None else _array(wk, dtype, D, "wk"))
 
 
 def lory_qk_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, freq: torch.Tensor,
@@ -449,25 +417,9 @@ def lory_qk_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, freq: torc
     """Head norms with weights wq, wk [head_dim] (none without them) and position rotation of q [tokens, q_heads,
     head_dim] and k [tokens, kv_heads, head_dim]; pos [tokens] int32, freq [rot_dim/2] fp64 radians per
     position.  Returns (q_out, k_out); an output may be its own input."""
-    qs, ks, dtype, hq, hk, ppos, pfreq, pwq, pwk = _rope_args(q, k, pos, freq, wq, wk)
-    if q_out is None:
-        q_out = torch.empty(qs, dtype=dtype, device=q.device)
-    if k_out is None:
-        k_out = torch.empty(ks, dtype=dtype, device=q.device)
-    shape = _rope_shape(q, k, 2 * freq.shape[0], eps, interleaved)
-    _check(lib().lory_qk_rope(shape, hq, hk, ppos, pfreq, pwq, pwk, _heads(q_out, dtype, qs, "q_out"),
-                              _heads(k_out, dtype, ks, "k_out"), _stream()), "lory_qk_rope")
+    status, q_out, k_out = _native().qk_rope(q, k, pos, freq, wq, wk, eps, interleaved, q_out, k_out)
+    _check(status, "lory_qk_rope")
     return q_out, k_out
-
-
-def _cache_dims(k_cache: torch.Tensor, v_cache: torch.Tensor, dtype: torch.dtype, Hkv: int, D: int) -> Tuple[int, int]:
-    shape = k_cache.shape
-    pages, heads, page, dim = shape
-    if heads != Hkv or dim != D or v_cache.shape != shape:
-        raise ValueError(f"k_cache and v_cache must be [pages, {Hkv}, page, {D}]")
-    if k_cache.dtype is not dtype or v_cache.dtype is not dtype:
-        raise TypeError(f"k_cache and v_cache must be {dtype}")
-    return pages, page
 
 
 def lory_qk_rope_cache(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, freq: torch.Tensor,
@@ -476,14 +428,8 @@ def lory_qk_rope_cache(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: t
                        wk: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False) -> torch.Tensor:
     """lory_qk_rope whose keys go, with the values v beside them, to slots [tokens] int64 of the caches [pages, kv_heads,
     page, head_dim] (slot = page number * page + row; outside of them: not stored).  Returns q_out."""
-    qs, ks, dtype, hq, hk, ppos, pfreq, pwq, pwk = _rope_args(q, k, pos, freq, wq, wk)
-    pages, page = _cache_dims(k_cache, v_cache, dtype, ks[1], ks[2])
-    if q_out is None:
-        q_out = torch.empty(qs, dtype=dtype, device=q.device)
-    shape = _rope_shape(q, k, 2 * freq.shape[0], eps, interleaved)
-    _check(lib().lory_qk_rope_cache(shape, hq, hk, _heads(v, dtype, ks, "v"), ppos, pfreq, pwq, pwk,
-                                    _heads(q_out, dtype, qs, "q_out"), _ptr(k_cache), _ptr(v_cache), pages, page,
-                                    _array(slots, torch.int64, ks[0], "slots"), _stream()), "lory_qk_rope_cache")
+    status, q_out = _native().qk_rope_cache(q, k, pos, freq, wq, wk, eps, interleaved, v, k_cache, v_cache, slots, q_out)
+    _check(status, "lory_qk_rope_cache")
     return q_out
 
 
@@ -506,29 +452,9 @@ def lory_qk_rope_bwd(q: torch.Tensor, k: torch.Tensor, dq_out: torch.Tensor, dk_
                      dwk: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(dq, dk, dwq, dwk) of lory_qk_rope from the gradients of its outputs; dwq, dwk [head_dim] fp32, None without weights.
     dq and dk may be dq_out and dk_out."""
-    qs, ks, dtype, hq, hk, ppos, pfreq, pwq, pwk = _rope_args(q, k, pos, freq, wq, wk)
-    if dq is None:
-        dq = torch.empty(qs, dtype=dtype, device=q.device)
-    if dk is None:
-        dk = torch.empty(ks, dtype=dtype, device=q.device)
-    D = q.shape[2]
-    if wq is not None:
-        if dwq is None:
-            dwq = torch.empty(D, dtype=torch.float32, device=q.device)
-        if dwk is None:
-            dwk = torch.empty(D, dtype=torch.float32, device=q.device)
-        if workspace is None:
-            workspace = alloc_qk_rope_workspace(q, k)
-    elif dwq is not None or dwk is not None:
-        raise ValueError("dwq and dwk need wq and wk")
-    shape = _rope_shape(q, k, 2 * freq.shape[0], eps, interleaved)
-    _check(lib().lory_qk_rope_bwd(shape, hq, hk, _heads(dq_out, dtype, qs, "dq_out"), _heads(dk_out, dtype, ks, "dk_out"),
-                                  ppos, pfreq, pwq, pwk, _heads(dq, dtype, qs, "dq"), _heads(dk, dtype, ks, "dk"),
-                                  None if dwq is None else _array(dwq, torch.float32, D, "dwq"),
-                                  None if dwk is None else _array(dwk, torch.float32, D, "dwk"), _ptr(workspace),
-                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()),
-           "lory_qk_rope_bwd")
-    return dq, dk, dwq, dwk
+    status, *grads = _native().qk_rope_bwd(q, k, pos, freq, wq, wk, eps, interleaved, dq_out, dk_out, dq, dk, dwq, dwk, workspace)
+    _check(status, "lory_qk_rope_bwd")
+    return tuple(grads)
 
 
 def lory_kv_plan(lens: torch.Tensor, add: torch.Tensor, table: torch.Tensor, free: torch.Tensor, count: torch.Tensor,
@@ -536,22 +462,9 @@ def lory_kv_plan(lens: torch.Tensor, add: torch.Tensor, table: torch.Tensor, fre
                  count_new: torch.Tensor, status: torch.Tensor) -> torch.Tensor:
     """Pages, positions and slots of a step's new tokens from the rows' lengths (add < 0: the row has ended), and the
     pages that come back; int32 but slots (int64).  Returns status [1]: 0, or why nothing was planned (include/lory.h)."""
-    B, F, room = lens.shape[0], free.shape[0], positions.shape[0]
-    i32 = torch.int32
-    ptable, width, table_row = _table(table, B)
-    _check(lib().lory_kv_plan(LoryPlanShape(B, width, page, F, room, table_row), _array(lens, i32, B, "lens"),
-                              _array(add, i32, B, "add"), ptable, _array(free, i32, F, "free"), _array(count, i32, 1, "count"),
-                              _array(lens_new, i32, B, "lens_new"), _array(cu, i32, B + 1, "cu"),
-                              _array(positions, i32, room, "positions"), _array(slots, torch.int64, room, "slots"),
-                              _array(count_new, i32, 1, "count_new"), _array(status, i32, 1, "status"), _stream()),
+    _check(_native().kv_plan(lens, add, table, free, count, page, lens_new, cu, positions, slots, count_new, status),
            "lory_kv_plan")
     return status
-
-
-def _paged_shape(q: torch.Tensor, k_cache: torch.Tensor, width: int, table_row: int, scale: float) -> LoryPagedShape:
-    B, Hq, D = q.shape
-    pages, Hkv, page, _ = k_cache.shape
-    return LoryPagedShape(B, Hq, Hkv, D, pages, page, width, _dtype_code(q.dtype), table_row, scale)
 
 
 def lory_paged_attn_workspace_bytes(shape: LoryPagedShape) -> int:
@@ -562,7 +475,10 @@ def lory_paged_attn_workspace_bytes(shape: LoryPagedShape) -> int:
 
 def alloc_paged_attn_workspace(q: torch.Tensor, k_cache: torch.Tensor, table: torch.Tensor) -> torch.Tensor:
     """Workspace of lory_paged_attn for these shapes."""
-    n = lory_paged_attn_workspace_bytes(_paged_shape(q, k_cache, table.shape[1], table.shape[1], 1.0))
+    B, Hq, D = q.shape
+    pages, Hkv, page, _ = k_cache.shape
+    width = table.shape[1]
+    n = lory_paged_attn_workspace_bytes(LoryPagedShape(B, Hq, Hkv, D, pages, page, width, _dtype_code(q.dtype), width, 1.0))
     return torch.empty(n, dtype=torch.uint8, device=q.device)
 
 
@@ -572,18 +488,6 @@ def lory_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     """out [rows, q_heads, head_dim] = attention of one token per row, q, over the first lens[b] tokens that table [rows,
     width] finds in the caches [pages, kv_heads, page, head_dim]; lse [rows, q_heads] fp32 receives the log of
     the sum of exponentials.  scale is 1/sqrt(head_dim) unless given."""
-    B, Hq, D = qs = q.shape
-    dtype = q.dtype
-    _cache_dims(k_cache, v_cache, dtype, k_cache.shape[1], D)
-    ptable, width, table_row = _table(table, B)
-    shape = _paged_shape(q, k_cache, width, table_row, D ** -0.5 if scale is None else scale)
-    if out is None:
-        out = torch.empty(qs, dtype=dtype, device=q.device)
-    if workspace is None:
-        workspace = alloc_paged_attn_workspace(q, k_cache, table)
-    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (B, Hq)):
-        raise ValueError(f"lse must be fp32 [{B}, {Hq}]")
-    _check(lib().lory_paged_attn(shape, _heads(q, dtype, qs, "q"), _ptr(k_cache), _ptr(v_cache), ptable,
-                                 _array(lens, torch.int32, B, "lens"), _heads(out, dtype, qs, "out"), _ptr(lse),
-                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()), "lory_paged_attn")
+    status, out = _native().paged_attn(q, k_cache, v_cache, table, lens, scale, out, lse, workspace)
+    _check(status, "lory_paged_attn")
     return out

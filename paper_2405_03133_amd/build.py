@@ -1,4 +1,4 @@
-"""Build liblory.so (the HIP library behind include/lory.h) for gfx950.
+"""Build liblory.so (the HIP library behind include/lory.h) for gfx950, and the extension module of its binding.
 
 Usage: python -m paper_2405_03133_amd.build
 The library is built in-tree next to this file so that it travels with the
@@ -98,6 +98,26 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
     return LIB
 
 
+MODULE = os.path.join(HERE, "_marshal.so")
+
+
+def build_marshal(verbose: bool = True) -> str:
+    """Compile csrc/marshal.cpp (host code against torch's and Python's headers) to the module _marshal beside liblory.so."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    libs = os.path.join(root, "lib")
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D__HIP_PLATFORM_AMD__",
+          "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, "-I", os.path.join(ROOT, "include"),
+          "-I", sysconfig.get_paths()["include"], "-I", os.path.join(root, "include"), "-I", os.path.join(rocm, "include"),
+          os.path.join(CSRC, "marshal.cpp"), "-o", MODULE, "-L", libs, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip",
+          "-L", HERE, "-l:liblory.so", "-Wl,-rpath,$ORIGIN"], verbose)
+    return MODULE
+
+
 if __name__ == "__main__":
     build()
+    build_marshal()
     sys.exit(0)

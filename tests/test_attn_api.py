@@ -195,28 +195,68 @@ def test_status_of_overlaps_has_a_text():
 # ---------------------------------------------------------------- the binding's own checks
 
 def test_binding_refuses_wrong_tensors():
+    """Types, shapes and strides are checked before devices, so CPU tensors reach every check."""
     q, k = torch.zeros(3, 4, 64), torch.zeros(3, 2, 64)
-    pos, freq = torch.zeros(3, dtype=torch.int32), torch.zeros(32, dtype=torch.float64)
-    with pytest.raises(ValueError, match="GPU"):
-        lb.lory_qk_rope(q, k, pos, freq)
-    with pytest.raises(ValueError, match="contiguous"):
-        lb.lory_qk_rope(q.transpose(1, 2).contiguous().transpose(1, 2), k, pos, freq)
-    with pytest.raises(TypeError, match="k must be"):
-        lb.lory_qk_rope(q.cuda() if torch.cuda.is_available() else _gpu_like(q), k.double(), pos, freq)
-    cache, table = torch.zeros(5, 2, 16, 64), torch.zeros(3, 4, dtype=torch.int32)
-    with pytest.raises(ValueError, match="k_cache"):
-        lb.lory_paged_attn(q, cache[..., :32], cache, table, pos)
-    with pytest.raises(TypeError, match="k_cache"):
-        lb.lory_paged_attn(q, cache.bfloat16(), cache, table, pos)
+    pos, freq, w = torch.zeros(3, dtype=torch.int32), torch.zeros(32, dtype=torch.float64), torch.ones(64)
 
+    def refused(error, match, f, *args, **kw):
+        with pytest.raises(error, match=match):
+            f(*args, **kw)
 
-class _gpu_like(torch.Tensor):
-    """A CPU tensor that claims to be on the GPU, for checks that come later than that one."""
-    @staticmethod
-    def __new__(cls, t):
-        return torch.Tensor._make_subclass(cls, t)
+    rope, bad = lb.lory_qk_rope, refused
+    bad(ValueError, "GPU", rope, q, k, pos, freq)
+    bad(ValueError, "last dimension of q .* contiguous", rope, torch.zeros(3, 4, 128)[..., ::2], k, pos, freq)
+    bad(TypeError, "k must be Float", rope, q, k.double(), pos, freq)
+    bad(TypeError, "unsupported dtype Half", rope, q.half(), k.half(), pos, freq)
+    bad(ValueError, r"k must be \[3, 2, 64\]", rope, q, k[..., :32], pos, freq)
+    bad(ValueError, "q and k must be", rope, q[0], k, pos, freq)
+    bad(ValueError, "pos must be Int", rope, q, k, pos.long(), freq)
+    bad(ValueError, "pos must be Int .3.", rope, q, k, pos[:2], freq)
+    bad(ValueError, "pos must be contiguous", rope, q, k, torch.zeros(6, dtype=torch.int32)[::2], freq)
+    bad(ValueError, "freq must be Double", rope, q, k, pos, freq.float())
+    bad(TypeError, "wq must be Float", rope, q, k, pos, freq, wq=w.bfloat16(), wk=w)
+    bad(ValueError, "wk must be Float .64.", rope, q, k, pos, freq, wq=w, wk=w[:32])
+    bad(ValueError, "q_out must be", rope, q, k, pos, freq, q_out=k)
+    bad(TypeError, "k_out must be", rope, q, k, pos, freq, k_out=k.bfloat16())
+    bad(TypeError, "q must be a tensor", rope, None, k, pos, freq)
+    bad(TypeError, "number", rope, q, k, pos, freq, eps="x")
+    bad(ValueError, "GPU", rope, torch.zeros(3, 4, 64, device="meta"), k, pos, freq)
 
-    is_cuda = True
+    cache, slots = torch.zeros(5, 2, 16, 64), torch.zeros(3, dtype=torch.int64)
+    store = lambda v=k, kc=cache, vc=cache, s=slots: lb.lory_qk_rope_cache(q, k, v, pos, freq, kc, vc, s)
+    bad(ValueError, "GPU", store)
+    bad(ValueError, "v must be", store, v=q)
+    bad(ValueError, "k_cache and v_cache must be", store, kc=cache[:, :1])
+    bad(ValueError, "k_cache and v_cache must be", store, vc=cache[:4])
+    bad(TypeError, "v_cache must be Float", store, vc=cache.bfloat16())
+    bad(ValueError, "k_cache must be contiguous", store, kc=torch.zeros(5, 2, 32, 64)[:, :, ::2])
+    bad(ValueError, "slots must be Long", store, s=slots.int())
+
+    grad = lb.lory_qk_rope_bwd
+    bad(ValueError, "GPU", grad, q, k, q, k, pos, freq, w, w)
+    bad(ValueError, "dk_out must be", grad, q, k, q, q, pos, freq)
+    bad(ValueError, "dwq and dwk need", grad, q, k, q, k, pos, freq, dwq=w)
+    bad(ValueError, "dwk must be Float .64.", grad, q, k, q, k, pos, freq, w, w, dwk=w[:1])
+
+    table = torch.zeros(3, 4, dtype=torch.int32)
+    attn = lb.lory_paged_attn
+    bad(ValueError, "GPU", attn, q, cache, cache, table, pos)
+    bad(ValueError, "k_cache and v_cache must be", attn, q, cache[..., :32], cache, table, pos)
+    bad(TypeError, "k_cache must be Float", attn, q, cache.bfloat16(), cache, table, pos)
+    bad(ValueError, "table must be int32", attn, q, cache, cache, table.long(), pos)
+    bad(ValueError, "table must be int32", attn, q, cache, cache, table[:2], pos)
+    bad(ValueError, "table must be int32", attn, q, cache, cache, torch.zeros(4, 3, dtype=torch.int32).T, pos)
+    bad(ValueError, "lens must be Int .3.", attn, q, cache, cache, table, pos[:1])
+    bad(ValueError, "lse must be fp32 .3, 4.", attn, q, cache, cache, table, pos, lse=torch.zeros(3, 2))
+    bad(TypeError, "out must be Float", attn, q, cache, cache, table, pos, out=q.double())
+
+    i = lambda n: torch.zeros(n, dtype=torch.int32)
+    args = [i(3), i(3), table, i(9), i(1), 16, i(3), i(4), i(8), torch.zeros(8, dtype=torch.int64), i(1), i(1)]
+    bad(ValueError, "GPU", lb.lory_kv_plan, *args)
+    for at, (wrong, match) in {1: (i(2), "add must be"), 4: (i(2), "count must be"), 7: (i(3), "cu must be Int .4."),
+                               9: (i(8), "slots must be Long"), 10: (i(1).long(), "count_new must be Int")}.items():
+        bad(ValueError, match, lb.lory_kv_plan, *args[:at], wrong, *args[at + 1:])
+    bad(ValueError, "page is too large", lb.lory_kv_plan, *args[:5], 1 << 40, *args[6:])
 
 
 # ---------------------------------------------------------------- index arithmetic
