@@ -31,7 +31,7 @@ template <typename T, int LPH, bool INTER, bool STORE> __global__ __launch_bound
     constexpr int VEC = 16 / sizeof(T), HPW = 64 / LPH;   // heads of a group: one load of the wavefront
     constexpr int U = 4;                                  // groups in flight
     __shared__ float2 table[kWaves][kMaxPairs];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = wave_index();
     const int t = blockIdx.x * kWaves + wave;
     if (t >= a.tokens) return;   // wavefronts share nothing
 
@@ -103,7 +103,7 @@ template <typename T, int LPH, bool INTER, bool STORE> __global__ __launch_bound
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) y[e] = r * fmaf(x[e], A[e], p[e] * B[e]);
                     if (h < H && l.on && write)
-                        *reinterpret_cast<Chunk *>(dst + h * dst_head + l.chunk * 16) = narrow<T>(y);
+                        store_once(dst + h * dst_head + l.chunk * 16, narrow<T>(y));
                 }
             }
         };
@@ -120,7 +120,7 @@ template <typename T, int LPH, bool INTER, bool STORE> __global__ __launch_bound
         for (int g = lo; g < g1 - gq - gk; ++g) {
             const int h = g * HPW + l.sub;
             if (h < a.Hkv)
-                *reinterpret_cast<Chunk *>(vrow + h * khead + l.chunk * 16) = *reinterpret_cast<const Chunk *>(src + h * a.v.head);
+                store_once(vrow + h * khead + l.chunk * 16, *reinterpret_cast<const Chunk *>(src + h * a.v.head));
         }
     }
 }

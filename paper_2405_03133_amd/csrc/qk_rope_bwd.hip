@@ -25,12 +25,12 @@ struct Args {
     float eps;
 };
 
-template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds__(64 * kWaves) void qk_rope_bwd_kernel(Args a)
+template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds__(64 * kWaves, 4) void qk_rope_bwd_kernel(Args a)
 {
     constexpr int VEC = 16 / sizeof(T), HPW = 64 / LPH, U = 2;
     __shared__ float2 table[kWaves][kMaxPairs];
     __shared__ float sums[kWaves][2 * LPH * VEC];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = wave_index();
     const Lane l = lane_of<T, LPH, INTER>(lane, a.D, a.rot);
     const int gq = (a.Hq + HPW - 1) / HPW, gk = (a.Hkv + HPW - 1) / HPW, groups = gq + gk;
 
@@ -61,8 +61,8 @@ template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds
                     const int h = (g + u) * HPW + l.sub;
                     rx[u] = rg[u] = Chunk{0, 0, 0, 0};
                     if (g + u < hi && h < H && l.on) {
-                        if constexpr (NORM) rx[u] = *reinterpret_cast<const Chunk *>(src + h * src_head + l.chunk * 16);
-                        rg[u] = *reinterpret_cast<const Chunk *>(grad + h * grad_head + l.chunk * 16);
+                        if constexpr (NORM) rx[u] = load_once(src + h * src_head + l.chunk * 16);
+                        rg[u] = load_once(grad + h * grad_head + l.chunk * 16);
                     }
                 }
 #pragma unroll
@@ -90,7 +90,7 @@ template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds
                             y[e] = r * fmaf(-x[e], m, y[e] * w[e]);
                         }
                     }
-                    if (h < H && l.on) *reinterpret_cast<Chunk *>(dst + h * dst_head + l.chunk * 16) = narrow<T>(y);
+                    if (h < H && l.on) store_once(dst + h * dst_head + l.chunk * 16, narrow<T>(y));
                 }
             }
         };
@@ -122,40 +122,49 @@ template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds
     }
 }
 
-// dw from the rows of partial sums: a wavefront of a workgroup takes every 16th row of 64 columns, and the 16 sums are added
-// in order.
+// dw from the rows of partial sums, 16 columns a workgroup: a thread takes every 64th row of its column, the 64 sums of a column
+// are added in order, a quarter per lane, and the quarters last.  1024 rows of 2 x 128: 2.4 us, bound by two latencies.
+constexpr int kDwColumns = 16;
+
 __global__ __launch_bounds__(1024) void qk_rope_dw_kernel(const float *part, int rows, int D, float *dwq, float *dwk)
 {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int col = blockIdx.x * 64 + lane;
+    __shared__ float sums[64][kDwColumns];
+    const int c = threadIdx.x % kDwColumns, g = threadIdx.x / kDwColumns;
+    const int col = blockIdx.x * kDwColumns + c;   // below 2 D, which is a multiple of 16
     float v = 0.f;
-    if (col < 2 * D) {
 #pragma unroll 8
-        for (int r = wave; r < rows; r += 16) v += part[(size_t)r * 2 * D + col];
-    }
-    sums[wave][lane] = v;
+    for (int r = g; r < rows; r += 64) v += part[(size_t)r * 2 * D + col];
+    sums[g][c] = v;
     __syncthreads();
-    if (wave != 0 || col >= 2 * D) return;
+    if (threadIdx.x >= 64) return;
     float total = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) total += sums[i][lane];
-    (col < D ? dwq : dwk)[col < D ? col : col - D] = total;
+    for (int i = 0; i < 16; ++i) total += sums[16 * g + i][c];
+    total += __shfl_xor(total, 16, 64);
+    total += __shfl_xor(total, 32, 64);
+    if (g == 0) (col < D ? dwq : dwk)[col < D ? col : col - D] = total;
 }
 
 struct Plan {
     int shares, blocks;
 };
 
-// A token's heads over several wavefronts until there are 4096 of them; then several tokens a wavefront.
+// A token's heads over as many wavefronts as end first: rounds of the items over 4 kMaxBlocks wavefronts, each as long as
+// its groups and about one more for the angles.
 Plan plan(const lory_rope_shape &s)
 {
     const int lph = s.dtype == LORY_F32 ? lanes_per_head<float>(s.head_dim) : lanes_per_head<__hip_bfloat16>(s.head_dim);
-    const int hpw = 64 / lph, groups = (s.q_heads + hpw - 1) / hpw + (s.kv_heads + hpw - 1) / hpw;
+    const int hpw = 64 / lph, groups = (s.q_heads + hpw - 1) / hpw + (s.kv_heads + hpw - 1) / hpw, waves = kWaves * kMaxBlocks;
     Plan p = {1, 0};
     if (s.tokens <= 0) return p;
-    long shares = (4 * kMaxBlocks + (long)s.tokens - 1) / s.tokens;
-    p.shares = (int)(shares < groups ? shares : groups);
+    long best = 0;
+    for (int n = 1; n <= groups && (n == 1 || (long)s.tokens * (n - 1) < 4 * waves); ++n) {
+        const long cost = ((long)s.tokens * n + waves - 1) / waves * ((groups + n - 1) / n + 1);
+        if (n == 1 || cost < best) {
+            best = cost;
+            p.shares = n;
+        }
+    }
     const long blocks = ((long)s.tokens * p.shares + kWaves - 1) / kWaves;
     p.blocks = (int)(blocks < kMaxBlocks ? blocks : kMaxBlocks);
     return p;
@@ -227,7 +236,7 @@ int qk_rope_bwd_launch(const lory_rope_shape &s, const lory_heads &q, const lory
             launch1<__hip_bfloat16>(a, p.blocks, inter, norm, st);
     }
     if (norm)
-        hipLaunchKernelGGL(qk_rope_dw_kernel, dim3((2 * s.head_dim + 63) / 64), dim3(1024), 0, st, (const float *)ws, p.blocks,
+        hipLaunchKernelGGL(qk_rope_dw_kernel, dim3(2 * s.head_dim / kDwColumns), dim3(1024), 0, st, (const float *)ws, p.blocks,
                            s.head_dim, dwq, dwk);
     return launch_status();
 }
