@@ -60,6 +60,7 @@ __global__ __launch_bounds__(kThreads) void kv_plan_kernel(Args a)
     __shared__ uint32_t wn[kWaves], wt[kWaves], wg[kWaves], wf[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int first = tid * a.chunk, last = min(first + a.chunk, a.rows);
+    const int32_t count = a.count[0];
 
     uint32_t n = 0, t = 0, g = 0, flags = 0;
     for (int b = first; b < last; ++b) {
@@ -106,7 +107,6 @@ __global__ __launch_bounds__(kThreads) void kv_plan_kernel(Args a)
     __syncthreads();
 
     const uint32_t tokens = pn[kThreads], taken = pt[kThreads], given = pg[kThreads];
-    const int32_t count = a.count[0];
     const int64_t top = (int64_t)count + given;
     if (count < 0 || count > a.free_size) flags |= 16;
     if (tokens > (uint32_t)a.room) flags |= 1;
@@ -155,46 +155,46 @@ __global__ __launch_bounds__(kThreads) void kv_plan_kernel(Args a)
         }
     }
 
-    for (long i = me; i < a.room; i += step) {
-        int64_t slot = -1;
-        int32_t at = 0;
-        if (ok && i < tokens) {
-            const int ch = chunk_of(pn, (uint32_t)i);
-            uint32_t rest = (uint32_t)i - pn[ch], took = pt[ch];
-            int b = ch * a.chunk;
-            const int end = min(b + a.chunk, a.rows) - 1;
-            int32_t len = a.lens[b];
-            Row r = row_of(a, len, a.add[b]);
-            while (b < end && rest >= r.n) {
-                rest -= r.n;
-                took += r.take;
-                ++b;
-                len = a.lens[b];
-                r = row_of(a, len, a.add[b]);
-            }
-            at = len + (int32_t)rest;
-            const uint32_t c = (uint32_t)at / (uint32_t)a.page;
-            const int32_t page = c < r.old ? a.table[(long)b * a.table_row + c] : stack(top - 1 - took - (c - r.old));
-            slot = (int64_t)page * a.page + (at - (int32_t)(c * a.page));
+    // one list of work: positions and slots, pages that rows take, places of the stack that pages come back to
+    const long back = ok && top - taken > count ? top - taken - count : 0, pages = ok ? taken : 0, all = a.room + pages + back;
+    for (long x = me; x < all; x += step) {
+        if (x >= a.room + pages) {
+            const int64_t j = count + (x - a.room - pages);
+            a.free[j] = stack(j);
+            continue;
         }
-        a.positions[i] = at;
-        a.slots[i] = slot;
-    }
-    if (!ok) return;
-    for (long i = me; i < taken; i += step) {
-        const int ch = chunk_of(pt, (uint32_t)i);
-        uint32_t rest = (uint32_t)i - pt[ch];
+        // the row of a token or of a page that is taken: rest items of it come before
+        const bool token = x < a.room;
+        const uint32_t i = (uint32_t)(token ? x : x - a.room);
+        if (token && (!ok || i >= tokens)) {
+            a.positions[i] = 0;
+            a.slots[i] = -1;
+            continue;
+        }
+        const int ch = token ? chunk_of(pn, i) : chunk_of(pt, i);
+        uint32_t rest = i - (token ? pn[ch] : pt[ch]), took = pt[ch];
         int b = ch * a.chunk;
         const int end = min(b + a.chunk, a.rows) - 1;
-        Row r = row_of(a, a.lens[b], a.add[b]);
-        while (b < end && rest >= r.take) {
-            rest -= r.take;
+        int32_t len = a.lens[b];
+        Row r = row_of(a, len, a.add[b]);
+        while (b < end && rest >= (token ? r.n : r.take)) {
+            rest -= token ? r.n : r.take;
+            took += r.take;
             ++b;
-            r = row_of(a, a.lens[b], a.add[b]);
+            len = a.lens[b];
+            r = row_of(a, len, a.add[b]);
         }
-        a.table[(long)b * a.table_row + r.old + rest] = stack(top - 1 - i);
+        int32_t *row = a.table + (long)b * a.table_row;
+        if (token) {
+            const int32_t at = len + (int32_t)rest;
+            const uint32_t c = (uint32_t)at / (uint32_t)a.page;
+            const int32_t page = c < r.old ? row[c] : stack(top - 1 - took - (c - r.old));
+            a.positions[i] = at;
+            a.slots[i] = (int64_t)page * a.page + (at - (int32_t)(c * a.page));
+        } else {
+            row[r.old + rest] = stack(top - 1 - i);
+        }
     }
-    for (int64_t j = count + me; j < top - (int64_t)taken; j += step) a.free[j] = stack(j);
 }
 
 }  // namespace
@@ -205,12 +205,10 @@ int kv_plan_launch(const lory_plan_shape &s, const int32_t *lens, const int32_t 
 {
     Args a = {lens, add, table, free, count, lens_new, cu, positions, slots, count_new, status,
               (long)s.table_row, s.rows, s.width, s.page, s.free_size, s.room, (s.rows + kThreads - 1) / kThreads};
-    // a token a thread, two workgroups a CU at most; many pages may come back where few tokens are new
-    long blocks = ((long)s.room + kThreads - 1) / kThreads;
-    const long pages = ((long)s.free_size + 4 * kThreads - 1) / (4 * kThreads);
-    if (blocks < pages) blocks = pages;
+    // a thread for every token, page that can be taken and place that one can come back to, two workgroups a CU at most
+    const long items = (long)s.room + s.room / s.page + s.rows + s.free_size;
+    long blocks = (items + kThreads - 1) / kThreads;
     if (blocks > 512) blocks = 512;
-    if (blocks < 1) blocks = 1;
     prof::Range r(st, prof::kKvPlan, 0.0, 12.0 * s.room + 16.0 * s.rows);
     hipLaunchKernelGGL(kv_plan_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, st, a);
     return launch_status();
