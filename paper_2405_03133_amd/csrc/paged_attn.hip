@@ -19,10 +19,10 @@
 // 2^-9, and the matrix cores wait for memory anyway.
 //
 // Pages: the lane that owns a key looks its page up two steps ahead; the others fetch the row by a lane permute.
+#include <hip/hip_bf16.h>
+
 #include "gemm_bf16.h"
 #include "lory_internal.h"
-
-#include "elem_io.h"
 #include "paged_index.h"
 
 namespace lory {
@@ -33,8 +33,11 @@ using gemm::bf16x8;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256, kWaves = 4;
-constexpr int kGroups = 512;   // workgroups that fill the chip: two on each of 256 CUs
+constexpr int kThreads = 256, kWaves = 4, kJoinThreads = 512;
+constexpr int kCUs = 256;
+// Workgroups of four wavefronts that the registers let a CU hold (heads of up to 64, 128, 256): 100 rows of 100 to 4000 tokens,
+// 8 heads of 64, in 512 ranges 58.8 us, in 768 52.2.
+constexpr int resident(int head_dim) { return head_dim <= 64 ? 3 : head_dim <= 128 ? 2 : 1; }
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Args {
@@ -48,7 +51,7 @@ struct Args {
     long out_row, out_head;   // bytes
     float *lse;
     int32_t *starts;          // workspace: units of one head before each row, [rows + 1]
-    float *part_o;            // pieces: [slots][part_rows][D]
+    float2 *part_o;           // pieces: [slots][part_rows][D / 2]
     float2 *part_ml;          // [slots][part_rows], maximum and sum
     int part_rows;
     int rows, Hq, Hkv, D, pages, page, width;
@@ -272,6 +275,18 @@ template <int DP, int NW> struct Shared {
     float m[NW][16], l[NW][16];
 };
 
+// Dims d and d + 1 of a query head's result from the sums relative to ref, and its lse with dim 0.
+template <typename T> __device__ __forceinline__ void write_out(const Args &a, int b, int head, int d, float ref, float L, float O0, float O1)
+{
+    const float n = L == 0.f ? 1.f : L;
+    char *p = a.out + b * a.out_row + head * a.out_head + d * (int)sizeof(T);
+    if constexpr (sizeof(T) == 2)
+        *reinterpret_cast<uint32_t *>(p) = gemm::cvt_pk_bf16(O0 / n, O1 / n);
+    else
+        *reinterpret_cast<float2 *>(p) = make_float2(O0 / n, O1 / n);
+    if (d == 0 && a.lse) a.lse[(long)b * a.Hq + head] = (ref + log2f(L)) * kLn2;
+}
+
 // Tiles t0 .. t1 of head h (a block of up to 16 query heads of a key-value head) of row b, whose length is len: the
 // wavefronts take turns of kKeys keys and join in LDS.  `whole`: the piece is all of the row, its result goes to out; else
 // it goes to slot `slot` of the workspace.
@@ -280,7 +295,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
 {
     using W = Wave<T, DP, PAD>;
     constexpr int KEYS = kKeys<T>, STEP = KEYS * NW, NS = KEYS / 4;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, c = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, c = lane >> 4;
     const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;   // first query head
     const int nq = min(16, (kvh + 1) * a.group - first);
     const int last = min(t1 * kTile<T>, len);
@@ -357,25 +372,27 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             for (int r = 0; r < 4; ++r) sh.o[wave][i][W::dim(t, 4 * c + r)] = w.o[t][r];
     }
     __syncthreads();
-    for (int x = tid; x < nq * a.D; x += 64 * NW) {
-        const int j = x / a.D, d = x - j * a.D;
+    const int pairs = a.D / 2;
+    for (int x = tid; x < nq * pairs; x += 64 * NW) {
+        const int j = x / pairs, d = (x - j * pairs) * 2;
         float M = sh.m[0][j];
 #pragma unroll
         for (int n = 1; n < NW; ++n) M = fmaxf(M, sh.m[n][j]);
         const float ref = M == -INFINITY ? 0.f : M;
-        float L = 0.f, O = 0.f;
+        float L = 0.f, O0 = 0.f, O1 = 0.f;
 #pragma unroll
         for (int n = 0; n < NW; ++n) {
             const float f = __builtin_amdgcn_exp2f(sh.m[n][j] - ref);
             L = fmaf(f, sh.l[n][j], L);
-            O = fmaf(f, sh.o[n][j][d], O);
+            O0 = fmaf(f, sh.o[n][j][d], O0);
+            O1 = fmaf(f, sh.o[n][j][d + 1], O1);
         }
         if (whole) {
-            Elem<T>::store((T *)(a.out + b * a.out_row + (first + j) * a.out_head) + d, O / (L == 0.f ? 1.f : L));
-            if (d == 0 && a.lse) a.lse[(long)b * a.Hq + first + j] = (ref + log2f(L)) * kLn2;
+            write_out<T>(a, b, first + j, d, ref, L, O0, O1);
         } else {
-            a.part_o[((long)slot * a.part_rows + j) * a.D + d] = O;
-            if (d == 0) a.part_ml[(long)slot * a.part_rows + j] = make_float2(M, L);
+            const long at = (long)slot * a.part_rows + j;
+            a.part_o[at * pairs + d / 2] = make_float2(O0, O1);
+            if (d == 0) a.part_ml[at] = make_float2(M, L);
         }
     }
     __syncthreads();
@@ -400,52 +417,49 @@ template <typename T, int DP, bool PAD, int NW> __global__ __launch_bounds__(64 
 template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Args a)
 {
     __shared__ Shared<DP, kWaves> sh;
-    __shared__ int sums[kThreads + 1], wsum[kWaves];
+    __shared__ int wsum[kWaves];
+    __shared__ struct { int row, len; long rest; } at;   // row of the range's first unit, and units of it before that
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int heads = a.Hkv * a.tiles;
 
-    // units of one head before each chunk of rows
-    const int chunk = (a.rows + kThreads - 1) / kThreads;
-    int n = 0;
-    for (int b = tid * chunk; b < min((tid + 1) * chunk, a.rows); ++b) n += units_of<T>(length_of(a, b));
+    // units of one head: of the thread's chunk of rows, then before it and of all rows
+    const int chunk = (a.rows + kThreads - 1) / kThreads, row0 = min(tid * chunk, a.rows), row1 = min(row0 + chunk, a.rows);
+    int own = 0;
+    for (int b = row0; b < row1; ++b) own += units_of<T>(length_of(a, b));
+    int upto = own;
     for (int m = 1; m < 64; m <<= 1) {
-        const int u = __shfl_up(n, m, 64);
-        if (lane >= m) n += u;
+        const int v = __shfl_up(upto, m, 64);
+        if (lane >= m) upto += v;
     }
-    if (lane == 63) wsum[wave] = n;
+    if (lane == 63) wsum[wave] = upto;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) n += wsum[w];
-    sums[tid + 1] = n;
-    if (tid == 0) sums[0] = 0;
-    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) upto += wsum[w];
+        total += wsum[w];
+    }
     if (blockIdx.x == 0) {   // for the launch that joins
-        n = sums[tid];
-        for (int b = tid * chunk; b < min((tid + 1) * chunk, a.rows); ++b) {
+        int n = upto - own;
+        for (int b = row0; b < row1; ++b) {
             a.starts[b] = n;
             n += units_of<T>(length_of(a, b));
         }
-        if (tid == 0) a.starts[a.rows] = sums[kThreads];
+        if (tid == 0) a.starts[a.rows] = total;
     }
-    const long U = (long)sums[kThreads] * heads;
+    const long U = (long)total * heads;
     long u = paged::range_begin(blockIdx.x, U, a.groups);
     const long end = paged::range_begin(blockIdx.x + 1, U, a.groups);
     if (u >= end) return;
-
-    // row, head and tile of the first unit
-    int lo = 0, hi = kThreads;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((long)sums[mid] * heads <= u) lo = mid; else hi = mid;
+    if ((long)(upto - own) * heads <= u && u < (long)upto * heads) {   // one thread's chunk has the range's first unit
+        long rest = u - (long)(upto - own) * heads;
+        int b = row0, len = length_of(a, b);
+        for (; b < row1 - 1 && rest >= (long)units_of<T>(len) * heads; len = length_of(a, ++b)) rest -= (long)units_of<T>(len) * heads;
+        at = {b, len, rest};
     }
-    int b = lo * chunk, len, units;
-    long rest = u - (long)sums[lo] * heads;
-    for (;; ++b) {
-        len = length_of(a, b);
-        units = units_of<T>(len);
-        if (rest < (long)units * heads || b == a.rows - 1) break;
-        rest -= (long)units * heads;
-    }
-    int h = (int)(rest / units), tile = (int)(rest - (long)h * units);
+    __syncthreads();
+    int b = at.row, len = at.len, units = units_of<T>(len);
+    int h = (int)(at.rest / units), tile = (int)(at.rest - (long)h * units);
 
     while (u < end) {
         const int stop = (int)(end - u < units - tile ? tile + (end - u) : units);
@@ -461,13 +475,12 @@ template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) v
     }
 }
 
-// Joins the pieces of one row's head, grid (heads, rows).  16 threads a query find the maximum and the sum; then every thread
-// adds four dims of one query over a share of the pieces, and the shares are added in order.  BY_ROW: the pieces are those of
-// paged_attn_rows_kernel.
-template <typename T, bool BY_ROW> __global__ __launch_bounds__(kThreads) void paged_attn_join_kernel(Args a)
+// Joins the pieces of one row's head, grid (heads, rows): every thread takes two dims of one query over a share of the pieces,
+// maximum, sum and output at once (one read of memory behind the row's place), and the shares are added in order.  BY_ROW:
+// the pieces are those of paged_attn_rows_kernel.
+template <typename T, bool BY_ROW> __global__ __launch_bounds__(kJoinThreads) void paged_attn_join_kernel(Args a)
 {
-    __shared__ float sm[16], sl[16];
-    __shared__ f32x4 so[kThreads];
+    __shared__ f32x4 scratch[kJoinThreads];
     const int h = blockIdx.x, heads = gridDim.x, tid = threadIdx.x;
     for (int b = blockIdx.y; b < a.rows; b += gridDim.y) {
         const int units = BY_ROW ? units_of<T>(length_of(a, b)) : a.starts[b + 1] - a.starts[b];
@@ -479,69 +492,48 @@ template <typename T, bool BY_ROW> __global__ __launch_bounds__(kThreads) void p
         const bool dense = U >= a.groups;
         const int parts = dense ? w1 - w0 + 1 : units;
         auto slot_of = [&](int p) {
-            const int w = dense ? w0 + p : paged::owner(u0 + p, U, a.groups);
+            const int w = dense ? w0 + p : (int)(((uint32_t)(u0 + p + 1) * a.groups - 1) / (uint32_t)U);   // owner, of fewer units
             return BY_ROW ? (b * heads + h) * a.groups + w : 2 * w + (p == 0);
         };
         const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;
         const int nq = min(16, (kvh + 1) * a.group - first);
 
-        const int j = tid >> 4, k = tid & 15;
-        float M = -INFINITY, L = 0.f;
-        if (j < nq)
-            for (int p = k; p < parts; p += 16) M = fmaxf(M, a.part_ml[(long)slot_of(p) * a.part_rows + j].x);
-#pragma unroll
-        for (int m = 1; m < 16; m <<= 1) M = fmaxf(M, __shfl_xor(M, m, 64));
-        const float ref = M == -INFINITY ? 0.f : M;
-        if (j < nq)
-            for (int p = k; p < parts; p += 16) {
-                const float2 ml = a.part_ml[(long)slot_of(p) * a.part_rows + j];
-                L = fmaf(__builtin_amdgcn_exp2f(ml.x - ref), ml.y, L);
-            }
-#pragma unroll
-        for (int m = 1; m < 16; m <<= 1) L += __shfl_xor(L, m, 64);
-        __syncthreads();   // the row before is done with the sums
-        if (j < nq && k == 0) {
-            sm[j] = ref;
-            sl[j] = L;
-            if (a.lse) a.lse[(long)b * a.Hq + first + j] = (ref + log2f(L)) * kLn2;
-        }
-        __syncthreads();
-
-        const int quads = a.D / 4, all = nq * quads;   // of all queries
-        int per = 16;                                  // threads that share a piece
-        while (per < all && per < kThreads) per <<= 1;
-        const int shares = kThreads / per, share = tid / per;
+        const int pairs = a.D / 2, all = nq * pairs;
+        int per = 16;   // threads that share a piece
+        while (per < all && per < kJoinThreads) per <<= 1;
+        const int shares = kJoinThreads / per, share = tid / per;
         for (int x0 = 0; x0 < all; x0 += per) {
             const int x = x0 + tid % per;
             const bool on = x < all;
-            const int jj = on ? x / quads : 0, d = on ? (x - jj * quads) * 4 : 0;
-            const float mref = sm[jj];
-            f32x4 O = {0.f, 0.f, 0.f, 0.f};
+            const int j = on ? x / pairs : 0, d = on ? x - j * pairs : 0;
+            float M = -INFINITY, L = 0.f, O0 = 0.f, O1 = 0.f;
+            auto take = [&](float m, float l, float o0, float o1) {
+                const float M1 = fmaxf(M, m), ref = M1 == -INFINITY ? 0.f : M1;
+                const float f = __builtin_amdgcn_exp2f(M - ref), g = __builtin_amdgcn_exp2f(m - ref);
+                L = L * f + l * g;
+                O0 = O0 * f + o0 * g;
+                O1 = O1 * f + o1 * g;
+                M = M1;
+            };
             if (on) {
-#pragma unroll 4
+#pragma unroll 8
                 for (int p = share; p < parts; p += shares) {
-                    const long slot = (long)slot_of(p) * a.part_rows + jj;
-                    const float f = __builtin_amdgcn_exp2f(a.part_ml[slot].x - mref);
-                    const f32x4 v = *reinterpret_cast<const f32x4 *>(a.part_o + slot * a.D + d);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) O[e] = fmaf(f, v[e], O[e]);
+                    const long at = (long)slot_of(p) * a.part_rows + j;
+                    const float2 ml = a.part_ml[at], o = a.part_o[at * pairs + d];
+                    take(ml.x, ml.y, o.x, o.y);
                 }
             }
             if (shares > 1) {
-                so[tid] = O;
+                scratch[tid] = f32x4{M, L, O0, O1};
                 __syncthreads();
                 if (share == 0)
-                    for (int n = 1; n < shares; ++n)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) O[e] += so[n * per + tid][e];
+                    for (int n = 1; n < shares; ++n) {
+                        const f32x4 v = scratch[n * per + tid];
+                        take(v[0], v[1], v[2], v[3]);
+                    }
                 __syncthreads();
             }
-            if (share == 0 && on) {
-                const float LL = sl[jj];
-                T *dst = (T *)(a.out + b * a.out_row + (first + jj) * a.out_head) + d;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) Elem<T>::store(dst + e, O[e] / (LL == 0.f ? 1.f : LL));
-            }
+            if (share == 0 && on) write_out<T>(a, b, first + j, 2 * d, M == -INFINITY ? 0.f : M, L, O0, O1);
         }
     }
 }
@@ -553,9 +545,11 @@ struct Plan {
 
 // How the units are cut, from the longest rows that the table allows (the lengths are on the device).  One workgroup takes
 // in about 60 bytes per ns, the second launch and the pieces cost 5 us:
-//  - a workgroup per row and head where that is at most 256 KB of keys and values, or up to 1 MB with so many rows that they
-//    fill the chip (us, one launch / cut; bf16, heads of 128: 2 heads of 512 tokens 8.8 / 9.1, of 1024 12.6 / 9.1; 64 of
-//    1024 14.5 / 14.1; 160 of 1024 17.1 / 23.2; 200 of 2048 41 / 50, of 4096 78 / 86);
+//  - a workgroup per row and head where that is at most 256 KB of keys and values, or up to 512 KB with so many rows that
+//    they fill the chip (us, one launch / cut; bf16, heads of 128: 2 heads of 512 tokens 8.8 / 8.7, of 1024 12.6 / 9.2; 64 of
+//    512 9.7 / 12.7, of 1024 14.3 / 14.6; 160 of 1024 16.6 / 21.9.  Beyond that the two are near each other, the cut
+//    behind where all rows are long and ahead where few are: 200 rows of 2048 42 / 50; 800 heads of 64 over 100 to 4000
+//    tokens 62 / 52);
 //  - every row cut alike where the ranges fill the chip once at most and the longest is short, so that it does not matter whose
 //    row is long (28 heads of up to 3001 tokens, fp32: 18.1 us, 20.4 with ranges over all rows; with longer ranges a
 //    ragged batch of 48 rows takes 46 us against 31);
@@ -566,10 +560,10 @@ Plan plan(const lory_paged_shape &s)
     const int group = s.q_heads / s.kv_heads;
     const long items = (long)s.rows * s.kv_heads * ((group + 15) / 16), most = ((long)s.width * s.page + tile - 1) / tile;
     const long row_bytes = 2 * most * tile * s.head_dim * esize, KB = 1024;
-    if (most == 1 || row_bytes <= 256 * KB || row_bytes <= (items < 128 ? items * 8 * KB : 1024 * KB)) return {1, 0};
-    const long n = items > 0 ? (kGroups / items < most ? kGroups / items : most) : 1;
+    if (most == 1 || row_bytes <= 256 * KB || row_bytes <= (items < 64 ? items * 8 * KB : 512 * KB)) return {1, 0};
+    const long n = items > 0 ? (2 * kCUs / items < most ? 2 * kCUs / items : most) : 1;
     if (n > 1 && row_bytes <= n * 256 * KB) return {(int)n, (int)(n * items)};
-    return {0, 2 * kGroups};
+    return {0, 2 * kCUs * resident(s.head_dim)};
 }
 
 template <typename T, int DP, bool PAD> void launch3(const Args &a, const Plan &p, hipStream_t st)
@@ -586,12 +580,12 @@ template <typename T, int DP, bool PAD> void launch3(const Args &a, const Plan &
             if (wide) hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 8>), grid, dim3(512), 0, st, g);
         }
         if (!wide) hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 4>), grid, dim3(256), 0, st, g);
-        if (p.ranges > 1) hipLaunchKernelGGL((paged_attn_join_kernel<T, true>), join, dim3(kThreads), 0, st, g);
+        if (p.ranges > 1) hipLaunchKernelGGL((paged_attn_join_kernel<T, true>), join, dim3(kJoinThreads), 0, st, g);
         return;
     }
-    g.groups = DP == 256 ? kGroups / 2 : kGroups;   // what the registers let run at a time
+    g.groups = kCUs * resident(DP);
     hipLaunchKernelGGL((paged_attn_kernel<T, DP, PAD>), dim3(g.groups), dim3(kThreads), 0, st, g);
-    hipLaunchKernelGGL((paged_attn_join_kernel<T, false>), join, dim3(kThreads), 0, st, g);
+    hipLaunchKernelGGL((paged_attn_join_kernel<T, false>), join, dim3(kJoinThreads), 0, st, g);
 }
 
 template <typename T, int DP> void launch2(const Args &a, const Plan &p, hipStream_t st)
@@ -653,8 +647,8 @@ int paged_attn_launch(const lory_paged_shape &s, const lory_heads &q, const void
     const Plan p = plan(s);
     a.starts = (int32_t *)ws;
     a.part_rows = part_rows(s);
-    a.part_o = (float *)((char *)ws + starts_bytes(s, p));
-    a.part_ml = (float2 *)(a.part_o + (size_t)p.slots * a.part_rows * s.head_dim);
+    a.part_o = (float2 *)((char *)ws + starts_bytes(s, p));
+    a.part_ml = a.part_o + (size_t)p.slots * a.part_rows * (s.head_dim / 2);
     a.rows = s.rows;
     a.Hq = s.q_heads;
     a.Hkv = s.kv_heads;
