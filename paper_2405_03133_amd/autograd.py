@@ -1,4 +1,5 @@
-"""torch.autograd wrapper of the Lory layer (Algorithm 1 of the paper and its gradient).
+"""torch.autograd wrappers: the Lory layer (Algorithm 1 of the paper and its gradient), and the norm and rotation of the
+query and key heads of the attention beside it (`qk_rope`).
 
 `lory_layer(x, R, Wg, Wu, Wd, T)` is what the paper's listing calls on the
 hidden states of a transformer block: route every segment on the previous
@@ -7,6 +8,8 @@ is computed by the HIP library through `binding`; this module only chains the
 entry points and hands torch the gradients (dX, dR, dWg, dWu, dWd).
 """
 from __future__ import annotations
+
+from typing import Optional
 
 import torch
 
@@ -60,3 +63,26 @@ def lory_layer(x: torch.Tensor, R: torch.Tensor, Wg: torch.Tensor, Wu: torch.Ten
         if lb.lory_merged_save_bytes(lb.make_shape(B, L, T, d, d_ff, E, x.dtype)) == 0:
             save_merged = False
     return _LoryLayer.apply(x, R, Wg, Wu, Wd, T, save_merged)
+
+
+class _QkRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, pos, freq, wq, wk, eps, interleaved):
+        ctx.save_for_backward(q, k, pos, freq, wq, wk)
+        ctx.eps, ctx.interleaved = eps, interleaved
+        return lb.lory_qk_rope(q, k, pos, freq, wq=wq, wk=wk, eps=eps, interleaved=interleaved)
+
+    @staticmethod
+    def backward(ctx, dq_out, dk_out):
+        q, k, pos, freq, wq, wk = ctx.saved_tensors
+        dq, dk, dwq, dwk = lb.lory_qk_rope_bwd(q, k, dq_out.contiguous(), dk_out.contiguous(), pos, freq, wq, wk, ctx.eps,
+                                               ctx.interleaved)
+        if wq is not None:
+            dwq, dwk = dwq.to(wq.dtype), dwk.to(wk.dtype)
+        return dq, dk, None, None, dwq, dwk, None, None
+
+
+def qk_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, freq: torch.Tensor, wq: Optional[torch.Tensor] = None,
+            wk: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False):
+    """(q_out, k_out) of binding.lory_qk_rope, differentiable in q, k, wq and wk."""
+    return _QkRope.apply(q, k, pos, freq, wq, wk, eps, interleaved)

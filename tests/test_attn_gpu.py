@@ -646,3 +646,105 @@ def test_on_another_stream_and_in_a_graph():
     # rows that have just ended keep stale pages in the table; their length is 0
     check_attention("last step", eager.out, eager.lse, eager.y, eager.k, eager.v, eager.table.clamp(min=0), eager.lens)
     assert max(n) > 5
+
+
+# ---------------------------------------------------------------- under autograd, and all together
+
+def test_autograd_of_norm_and_rotation():
+    """Leaves of one product, shared heads by expansion, an output that is not used: against autograd of the formula."""
+    from paper_2405_03133_amd.autograd import qk_rope
+    g = gen(12)
+    n, Hq, Hkv, D = 19, 6, 2, 64
+    base = rnd(g, n, (Hq + Hkv) * D)
+    wq, wk = 1 + 0.3 * rnd(g, D), 1 + 0.3 * rnd(g, D)
+    pos, freq = torch.randint(0, 999, (n,), device="cuda", dtype=torch.int32), freqs(D)
+    c = rnd(g, n, Hq, D)
+
+    def grads(f, dtype, only_q, shared):
+        x, a, b = (t.to(dtype).requires_grad_() for t in (base, wq, wk))
+        q, k = (t.unflatten(1, (-1, D)) for t in x.split([Hq * D, Hkv * D], 1))
+        if shared:
+            q = q[:, :1].expand(n, Hq, D)
+        yq, yk = f(q, k, a, b)
+        loss = (yq * c.to(dtype)).sum()
+        if not only_q:
+            loss = loss + yk.sum()   # its gradient is an expanded one
+        return torch.autograd.grad(loss, [x, a, b], allow_unused=True)
+
+    def formula(q, k, a, b):
+        f = lambda x, w: turned(x / (x.square().mean(-1, keepdim=True) + EPS).sqrt() * w, pos, freq, False)
+        return f(q, a), f(k, b)
+
+    for only_q in (False, True):
+        for shared in (False, True):
+            got = grads(lambda q, k, a, b: qk_rope(q, k, pos, freq, a, b, EPS), torch.float32, only_q, shared)
+            ref = grads(formula, torch.float64, only_q, shared)
+            for name, a, b in zip(("x", "wq", "wk"), got, ref):
+                b = torch.zeros_like(a, dtype=torch.float64) if b is None else b
+                # sums of up to 6 * 19 terms of order 1, 48 * 2^-24 of each
+                assert (a.double() - b).abs().max().item() <= 48 * E32 * 114 * max(1.0, b.abs().max().item()), (name, only_q, shared)
+
+
+def test_generation_example():
+    """The example's block over prompts of different lengths and eight steps in which one request ends, in fp32 against the
+    same block in 64 bits (the bars of the layer's fp32 configuration)."""
+    import importlib.util
+    import os
+
+    from parity_util import check, host
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "generate_block.py")
+    spec = importlib.util.spec_from_file_location("generate_block", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    block = ex.Block(d=128, heads=6, kv_heads=2, head_dim=64, d_ff=192, experts=4, dtype=torch.float32)
+    B, L, steps, page = 5, 37, 8, 8
+    requests = ex.Requests(block, B, B * 6, page, L + steps)
+    lens = torch.tensor([37, 1, 8, 20, 9], device="cuda", dtype=torch.int32)
+    prompts = rnd(gen(21), B, L, block.d)
+
+    W = {n: getattr(block, n).double() for n in ("Wqkv", "Wo", "wq", "wk", "R", "Wg", "Wu", "Wd")}
+    H, Hkv, D = block.H, block.Hkv, block.D
+
+    def ffn(x, m):
+        a, b = x @ m[0], x @ m[1]
+        return (a * torch.sigmoid(a) * b) @ m[2]
+
+    def plain(x, past, m):
+        """Tokens x [n, d] behind the request's cached (k, v); all in 64 bits."""
+        n, at = x.shape[0], 0 if past is None else past[0].shape[0]
+        q, k, v = (t.unflatten(1, (-1, D)) for t in (x @ W["Wqkv"]).split([H * D, Hkv * D, Hkv * D], 1))
+        pos = torch.arange(at, at + n, device="cuda")
+        norm = lambda t, w: turned(t / (t.square().mean(-1, keepdim=True) + 1e-6).sqrt() * w, pos, block.freq, False)
+        q, k = norm(q, W["wq"]), norm(k, W["wk"])
+        if past is not None:
+            k, v = torch.cat([past[0], k]), torch.cat([past[1], v])
+        out = torch.empty(n, H, D, dtype=torch.float64, device="cuda")
+        for h in range(H):
+            z = q[:, h] @ k[:, h // 3].T * D ** -0.5
+            z = z.masked_fill(torch.arange(at + n, device="cuda")[None] > pos[:, None], float("-inf"))
+            out[:, h] = torch.softmax(z, -1) @ v[:, h // 3]
+        y = x + out.flatten(1) @ W["Wo"]
+        return y + ffn(y, m), (k, v)
+
+    h, merged = ex.prefill(block, requests, prompts, lens)
+    ref, x64 = [], []
+    for b, n in enumerate(lens.tolist()):
+        e = torch.softmax(prompts[b, :n].double().mean(0) @ W["R"], -1)
+        m = [torch.tensordot(e, W[k], 1) for k in ("Wg", "Wu", "Wd")]
+        y, past = plain(prompts[b, :n].double(), None, m)
+        check(f"prompt of {n}", host(h[b, :n]), y.cpu().numpy(), 1e-5)
+        ref.append((past, m))
+    x = ex.next_input(h[torch.arange(B, device="cuda"), lens.long() - 1])
+    active = torch.ones(B, dtype=torch.bool, device="cuda")
+    for step in range(steps):
+        if step == 4:
+            active[2] = False
+        out = ex.decode(block, requests, x, active, merged)
+        for b in range(B):
+            if active[b]:
+                y, past = plain(x[b:b + 1].double(), ref[b][0], ref[b][1])
+                check(f"step {step} request {b}", host(out[b:b + 1]), y.cpu().numpy(), 1e-5)
+                ref[b] = (past, ref[b][1])
+        x = torch.where(active[:, None], ex.next_input(out), x)
+    assert requests.lens.tolist() == [45, 9, 0, 28, 17] and requests.status.item() == 0
+    assert requests.count.item() == B * 6 - (6 + 2 + 4 + 3)
