@@ -95,9 +95,11 @@ template <int DP, bool PAD> struct Wave<__hip_bfloat16, DP, PAD> {
     static constexpr int NT = DP / 16;     // output tiles
     static constexpr int VW = NT < 8 ? NT : 8;   // dims of a V load
     static constexpr int VL = NT / VW;     // V loads of a key
+    struct Keys {   // of a step
+        u32x4 k[2][KS];
+        uint32_t v[8][VL][VW / 2];
+    };
     bf16x8 q[KS];
-    u32x4 k[2][KS];
-    uint32_t v[8][VL][VW / 2];
     f32x4 o[NT];
 
     // dim of row i of output tile t
@@ -113,56 +115,56 @@ template <int DP, bool PAD> struct Wave<__hip_bfloat16, DP, PAD> {
         }
     }
     // row: of the lane's own key of the step (lane & 31)
-    __device__ void load_k(const char *base, int row, int D, int i, int c)
+    __device__ static void load_k(Keys &x, const char *base, int row, int D, int i, int c)
     {
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
-            const long r = __shfl(row, kt * 16 + i, 64);
-            const char *p = base + r * (D * 2) + c * 16;
+            const uint32_t r = __shfl(row, kt * 16 + i, 64);
+            const char *p = base + (uint64_t)r * (uint32_t)(PAD ? D * 2 : DP * 2) + c * 16;
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                if (PAD) k[kt][s] = u32x4{0, 0, 0, 0};
-                if (!PAD || (4 * s + c) * 8 < D) k[kt][s] = *reinterpret_cast<const u32x4 *>(p + s * 64);
+                if (PAD) x.k[kt][s] = u32x4{0, 0, 0, 0};
+                if (!PAD || (4 * s + c) * 8 < D) x.k[kt][s] = *reinterpret_cast<const u32x4 *>(p + s * 64);
             }
         }
     }
-    __device__ void load_v(const char *base, int row, int D, int i, int c)
+    __device__ static void load_v(Keys &x, const char *base, int row, int D, int i, int c)
     {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const long r = __shfl(row, (j >> 2) * 16 + 4 * c + (j & 3), 64);
-            const char *p = base + r * (D * 2) + i * (VW * 2);
+            const uint32_t r = __shfl(row, (j >> 2) * 16 + 4 * c + (j & 3), 64);
+            const char *p = base + (uint64_t)r * (uint32_t)(PAD ? D * 2 : DP * 2) + i * (VW * 2);
 #pragma unroll
             for (int m = 0; m < VL; ++m) {
                 if constexpr (VW == 8) {
-                    u32x4 x = {0, 0, 0, 0};
-                    if (!PAD || (16 * m + i) * 8 < D) x = *reinterpret_cast<const u32x4 *>(p + m * 256);
+                    u32x4 y = {0, 0, 0, 0};
+                    if (!PAD || (16 * m + i) * 8 < D) y = *reinterpret_cast<const u32x4 *>(p + m * 256);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[j][m][e] = x[e];
+                    for (int e = 0; e < 4; ++e) x.v[j][m][e] = y[e];
                 } else {
-                    uint2 x = {0, 0};
-                    if (!PAD || i * 4 < D) x = *reinterpret_cast<const uint2 *>(p);
-                    v[j][m][0] = x.x;
-                    v[j][m][1] = x.y;
+                    uint2 y = {0, 0};
+                    if (!PAD || i * 4 < D) y = *reinterpret_cast<const uint2 *>(p);
+                    x.v[j][m][0] = y.x;
+                    x.v[j][m][1] = y.y;
                 }
             }
         }
     }
     // s[n]: score of the lane's query with key (n / 4) * 16 + 4c + n % 4
-    __device__ void scores(float (&s)[8])
+    __device__ void scores(const Keys &x, float (&s)[8])
     {
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < KS; ++t)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[kt][t]), q[t], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[kt][t]), q[t], acc, 0, 0, 0);
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[kt * 4 + r] = acc[r];
         }
     }
     // the values of keys that are left out have no bits that may enter a product
-    __device__ void clear_v(uint32_t valid, int c)
+    __device__ static void clear_v(Keys &x, uint32_t valid, int c)
     {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -170,10 +172,10 @@ template <int DP, bool PAD> struct Wave<__hip_bfloat16, DP, PAD> {
 #pragma unroll
             for (int m = 0; m < VL; ++m)
 #pragma unroll
-                for (int e = 0; e < VW / 2; ++e) v[j][m][e] = on ? v[j][m][e] : 0;
+                for (int e = 0; e < VW / 2; ++e) x.v[j][m][e] = on ? x.v[j][m][e] : 0;
         }
     }
-    __device__ void add(const float (&p)[8])
+    __device__ void add(const Keys &x, const float (&p)[8])
     {
         u32x4 hi, lo;
 #pragma unroll
@@ -184,12 +186,12 @@ template <int DP, bool PAD> struct Wave<__hip_bfloat16, DP, PAD> {
         const bf16x8 bh = __builtin_bit_cast(bf16x8, hi), bl = __builtin_bit_cast(bf16x8, lo);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            u32x4 x;
+            u32x4 y;
 #pragma unroll
             for (int n = 0; n < 4; ++n)
-                x[n] = __builtin_amdgcn_perm(v[2 * n + 1][t / VW][(t % VW) / 2], v[2 * n][t / VW][(t % VW) / 2],
+                y[n] = __builtin_amdgcn_perm(x.v[2 * n + 1][t / VW][(t % VW) / 2], x.v[2 * n][t / VW][(t % VW) / 2],
                                              (t & 1) ? 0x07060302u : 0x05040100u);
-            const bf16x8 af = __builtin_bit_cast(bf16x8, x);
+            const bf16x8 af = __builtin_bit_cast(bf16x8, y);
             o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af, bh, o[t], 0, 0, 0);
             o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af, bl, o[t], 0, 0, 0);
         }
@@ -200,9 +202,11 @@ template <int DP, bool PAD> struct Wave<float, DP, PAD> {
     static constexpr int KS = DP / 16;   // 16-byte pieces of a key per lane
     static constexpr int NT = DP / 16;
     static constexpr int VL = DP / 64;
+    struct Keys {   // of a step
+        f32x4 k[KS];
+        f32x4 v[4][VL];
+    };
     f32x4 q[KS];
-    f32x4 k[KS];
-    f32x4 v[4][VL];
     f32x4 o[NT];
 
     static __device__ int dim(int t, int i) { return (t / 4) * 64 + 4 * i + t % 4; }
@@ -215,40 +219,40 @@ template <int DP, bool PAD> struct Wave<float, DP, PAD> {
             if (on && (!PAD || (4 * s + c) * 4 < D)) q[s] = *reinterpret_cast<const f32x4 *>(p + (4 * s + c) * 16);
         }
     }
-    __device__ void load_k(const char *base, int row, int D, int i, int c)
+    __device__ static void load_k(Keys &x, const char *base, int row, int D, int i, int c)
     {
-        const long r = __shfl(row, i, 64);
-        const char *p = base + r * (D * 4) + c * 16;
+        const uint32_t r = __shfl(row, i, 64);
+        const char *p = base + (uint64_t)r * (uint32_t)(PAD ? D * 4 : DP * 4) + c * 16;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            if (PAD) k[s] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (!PAD || (4 * s + c) * 4 < D) k[s] = *reinterpret_cast<const f32x4 *>(p + s * 64);
+            if (PAD) x.k[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (!PAD || (4 * s + c) * 4 < D) x.k[s] = *reinterpret_cast<const f32x4 *>(p + s * 64);
         }
     }
-    __device__ void load_v(const char *base, int row, int D, int i, int c)
+    __device__ static void load_v(Keys &x, const char *base, int row, int D, int i, int c)
     {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const long r = __shfl(row, 4 * c + j, 64);
-            const char *p = base + r * (D * 4) + i * 16;
+            const uint32_t r = __shfl(row, 4 * c + j, 64);
+            const char *p = base + (uint64_t)r * (uint32_t)(PAD ? D * 4 : DP * 4) + i * 16;
 #pragma unroll
             for (int m = 0; m < VL; ++m) {
-                if (PAD) v[j][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (!PAD || (16 * m + i) * 4 < D) v[j][m] = *reinterpret_cast<const f32x4 *>(p + m * 256);
+                if (PAD) x.v[j][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (!PAD || (16 * m + i) * 4 < D) x.v[j][m] = *reinterpret_cast<const f32x4 *>(p + m * 256);
             }
         }
     }
-    __device__ void scores(float (&s)[4])
+    __device__ void scores(const Keys &x, float (&s)[4])
     {
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < KS; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(k[t][e], q[t][e], acc, 0, 0, 0);
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.k[t][e], q[t][e], acc, 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[r] = acc[r];
     }
-    __device__ void clear_v(uint32_t valid, int c)
+    __device__ static void clear_v(Keys &x, uint32_t valid, int c)
     {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -256,16 +260,16 @@ template <int DP, bool PAD> struct Wave<float, DP, PAD> {
 #pragma unroll
             for (int m = 0; m < VL; ++m)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[j][m][e] = on ? v[j][m][e] : 0.f;
+                for (int e = 0; e < 4; ++e) x.v[j][m][e] = on ? x.v[j][m][e] : 0.f;
         }
     }
-    __device__ void add(const float (&p)[4])
+    __device__ void add(const Keys &x, const float (&p)[4])
     {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[j][t / 4][t % 4], p[j], o[t], 0, 0, 0);
+                o[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x.v[j][t / 4][t % 4], p[j], o[t], 0, 0, 0);
     }
 };
 
@@ -296,7 +300,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
     using W = Wave<T, DP, PAD>;
     constexpr int KEYS = kKeys<T>, STEP = KEYS * NW, NS = KEYS / 4;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, c = lane >> 4;
-    const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;   // first query head
+    const int kvh = a.tiles == 1 ? h : h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;   // first query head
     const int nq = min(16, (kvh + 1) * a.group - first);
     const int last = min(t1 * kTile<T>, len);
 
@@ -310,6 +314,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
     auto row_of = [&](int at, int page) {
         return paged::cache_row(a.div, at + (lane & (KEYS - 1)), page, a.pages, a.Hkv, kvh);
     };
+    typename W::Keys x;
     int at = t0 * kTile<T> + wave * KEYS;
     int page = page_of(at), next = page_of(at + STEP);
     w.load_q(a.q + b * a.q_row + (first + i) * a.q_head, a.D, c, i < nq);
@@ -319,25 +324,32 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
 
     int row = row_of(at, page);
     if (at < last) {
-        w.load_k(a.k, max(row, 0), a.D, i, c);
-        w.load_v(a.v, max(row, 0), a.D, i, c);
+        W::load_k(x, a.k, max(row, 0), a.D, i, c);
+        W::load_v(x, a.v, max(row, 0), a.D, i, c);
     }
     for (; at < last; at += STEP) {
-        const uint32_t valid = (uint32_t)__ballot(row >= 0);
-        const int row1 = row_of(at + STEP, next);
+#pragma clang fp contract(off)
+        const uint32_t valid = (uint32_t)__ballot(row >= 0), every = (uint32_t)((1ull << KEYS) - 1);
+        row = row_of(at + STEP, next);
         next = page_of(at + 2 * STEP);
         const bool more = at + STEP < last;
 
         float s[NS];
-        w.scores(s);
-        if (more) w.load_k(a.k, max(row1, 0), a.D, i, c);
+        w.scores(x, s);
+        if (more) W::load_k(x, a.k, max(row, 0), a.D, i, c);
 
-        float top = -INFINITY;
+        // rounded before the maximum is taken off: equal scores of any size stay equal (a fused product would not)
 #pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            s[n] = (valid >> ((n >> 2) * 16 + 4 * c + (n & 3))) & 1 ? s[n] * a.scale2 : -INFINITY;
-            top = fmaxf(top, s[n]);
+        for (int n = 0; n < NS; ++n) s[n] *= a.scale2;
+        if (valid != every) {
+            W::clear_v(x, valid, c);
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+                if (!((valid >> ((n >> 2) * 16 + 4 * c + (n & 3))) & 1)) s[n] = -INFINITY;
         }
+        float top = s[0];
+#pragma unroll
+        for (int n = 1; n < NS; ++n) top = fmaxf(top, s[n]);
         const float m1 = fmaxf(m, xor_max(top));
         const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing but -inf so far: every weight is 0
         if (__any(m1 != m)) {
@@ -346,7 +358,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
 #pragma unroll
             for (int t = 0; t < W::NT; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) w.o[t][r] *= f;
+                for (int e = 0; e < 4; ++e) w.o[t][e] *= f;
         }
         m = m1;
 #pragma unroll
@@ -354,10 +366,8 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             s[n] = __builtin_amdgcn_exp2f(s[n] - ref);
             l += s[n];
         }
-        if (valid != (uint32_t)((1ull << KEYS) - 1)) w.clear_v(valid, c);
-        w.add(s);
-        if (more) w.load_v(a.v, max(row1, 0), a.D, i, c);
-        row = row1;
+        w.add(x, s);
+        if (more) W::load_v(x, a.v, max(row, 0), a.D, i, c);
     }
     l = xor_sum(l);
 
@@ -398,18 +408,16 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
     __syncthreads();
 }
 
-// A row's units in a.groups equal ranges, a workgroup each (one range: all of the row, and nothing is left to join).
+// A row's units in equal ranges, a workgroup each: grid (ranges, heads, rows).  One range: all of the row, and nothing is left
+// to join.
 template <typename T, int DP, bool PAD, int NW> __global__ __launch_bounds__(64 * NW) void paged_attn_rows_kernel(Args a)
 {
     __shared__ Shared<DP, NW> sh;
-    const int heads = a.Hkv * a.tiles, S = a.groups;
-    const long all = (long)a.rows * heads * S;
-    for (long x = blockIdx.x; x < all; x += gridDim.x) {
-        const long item = x / S;
-        const int s = (int)(x - item * S), b = (int)(item / heads), h = (int)(item - (long)b * heads);
+    const int s = blockIdx.x, S = gridDim.x, h = blockIdx.y;
+    for (int b = blockIdx.z; b < a.rows; b += gridDim.z) {
         const int len = length_of(a, b), units = units_of<T>(len);
-        const int t0 = (int)paged::range_begin(s, units, S), t1 = (int)paged::range_begin(s + 1, units, S);
-        if (t0 < t1) piece<T, DP, PAD, NW>(a, sh, b, h, t0, t1, len, t0 == 0 && t1 == units, (int)x);
+        const int t0 = S == 1 ? 0 : (int)paged::range_begin(s, units, S), t1 = S == 1 ? units : (int)paged::range_begin(s + 1, units, S);
+        if (t0 < t1) piece<T, DP, PAD, NW>(a, sh, b, h, t0, t1, len, t0 == 0 && t1 == units, (b * (int)gridDim.y + h) * S + s);
     }
 }
 
@@ -448,8 +456,9 @@ template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) v
         if (tid == 0) a.starts[a.rows] = total;
     }
     const long U = (long)total * heads;
-    long u = paged::range_begin(blockIdx.x, U, a.groups);
-    const long end = paged::range_begin(blockIdx.x + 1, U, a.groups);
+    constexpr int groups = kCUs * resident(DP);
+    long u = paged::range_begin(blockIdx.x, U, groups);
+    const long end = paged::range_begin(blockIdx.x + 1, U, groups);
     if (u >= end) return;
     if ((long)(upto - own) * heads <= u && u < (long)upto * heads) {   // one thread's chunk has the range's first unit
         long rest = u - (long)(upto - own) * heads;
@@ -459,7 +468,7 @@ template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) v
     }
     __syncthreads();
     int b = at.row, len = at.len, units = units_of<T>(len);
-    int h = (int)(at.rest / units), tile = (int)(at.rest - (long)h * units);
+    int h = (int)paged::quotient64(at.rest, units), tile = (int)(at.rest - (long)h * units);
 
     while (u < end) {
         const int stop = (int)(end - u < units - tile ? tile + (end - u) : units);
@@ -495,7 +504,7 @@ template <typename T, bool BY_ROW> __global__ __launch_bounds__(kJoinThreads) vo
             const int w = dense ? w0 + p : (int)(((uint32_t)(u0 + p + 1) * a.groups - 1) / (uint32_t)U);   // owner, of fewer units
             return BY_ROW ? (b * heads + h) * a.groups + w : 2 * w + (p == 0);
         };
-        const int kvh = h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;
+        const int kvh = a.tiles == 1 ? h : h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;
         const int nq = min(16, (kvh + 1) * a.group - first);
 
         const int pairs = a.D / 2, all = nq * pairs;
@@ -573,7 +582,7 @@ template <typename T, int DP, bool PAD> void launch3(const Args &a, const Plan &
     if (p.ranges) {
         g.groups = p.ranges;
         const long all = (long)a.rows * a.Hkv * a.tiles * p.ranges;
-        const dim3 grid((unsigned)(all < 65536 ? all : 65536));
+        const dim3 grid(p.ranges, a.Hkv * a.tiles, a.rows < 65535 ? a.rows : 65535);
         bool wide = false;
         if constexpr (DP <= 128) {   // eight wavefronts of the widest heads would spill
             wide = all <= 256;
