@@ -193,9 +193,9 @@ def lory_profile_enable(on: bool) -> None:
 
 def lory_profile_read() -> list:
     """Per kernel class: dict(name, launches, ms, flops, bytes) since the last read."""
-    buf = (LoryKernelStat * 16)()
+    buf = (LoryKernelStat * 32)()
     n = ctypes.c_int(0)
-    _check(lib().lory_profile_read(buf, 16, ctypes.byref(n)), "lory_profile_read")
+    _check(lib().lory_profile_read(buf, 32, ctypes.byref(n)), "lory_profile_read")
     return [dict(name=buf[i].name.decode(), launches=buf[i].launches, ms=buf[i].ms, flops=buf[i].flops,
                  bytes=buf[i].bytes) for i in range(n.value)]
 

@@ -5,6 +5,12 @@
 // are enough tokens to fill the chip, a share of them otherwise), so the token's angles are formed once, one pair
 // per lane, and stay in registers as the factors of the lane's values, with the norm's weights multiplied in:
 //   y_e = r (x_e (w_e c_e) + p_e (w'_e s_e)),   r = 1 / sqrt(mean + eps).
+// Four groups of heads are loaded at a time; two or eight were slower (16384 tokens of 32 heads of 128, bf16: 55.4 and 54.9 us
+// against 52.1), and so was loading queries, keys and values before the angles are formed (57.4: the registers for it cost two
+// of six wavefronts per SIMD).
+// Measured: those 16384 tokens 50.6 us, 5.3 TB/s; prompts of 12001 tokens (16 + 4 heads) into the cache 25.7 us, 5.7 TB/s; 4093
+// fp32 tokens (16 heads of 80, 20 of 32 lanes in use) 11.1 us, 3.8 TB/s; 48 tokens into the cache 4.2 us, of which a launch
+// that does nothing takes 1.8.  HBM traffic is that of the heads alone (134.9 + 134.2 MB of 268.5).
 #include "qk_rope.h"
 
 namespace lory {
@@ -130,7 +136,8 @@ template <typename T, int LPH, bool STORE> void launch2(const Args &a, bool inte
     constexpr int HPW = 64 / LPH;
     const int gq = (a.Hq + HPW - 1) / HPW, gk = (a.Hkv + HPW - 1) / HPW;
     const int groups = gq + gk * (STORE ? 2 : 1), blocks = (a.tokens + kWaves - 1) / kWaves;
-    // a token's heads over several wavefronts until there are 4096 of them (four per SIMD)
+    // a token's heads over several wavefronts until there are 4096 of them (four per SIMD; 48 tokens of 40 heads take 4.2 us
+    // so, and more wavefronts cost larger calls the angles again: 4093 fp32 tokens 15.7 us against 11.3)
     int ny = (1024 + blocks - 1) / blocks;
     if (ny > groups) ny = groups;
     const dim3 grid(blocks, ny);

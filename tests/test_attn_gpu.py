@@ -648,6 +648,27 @@ def test_on_another_stream_and_in_a_graph():
     assert max(n) > 5
 
 
+def test_event_timing_knows_the_operators():
+    n, H, D, page = 64, 4, 64, 16
+    x, pos, freq, w = rnd(gen(0), n, H, D), torch.zeros(n, dtype=torch.int32, device="cuda"), freqs(D), torch.ones(D, device="cuda")
+    cache = torch.zeros(8, H, page, D, device="cuda")
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    lb.lory_profile_read()
+    lb.lory_profile_enable(True)
+    try:
+        lb.lory_qk_rope(x, x, pos, freq)
+        lb.lory_qk_rope_bwd(x, x, x, x, pos, freq, w, w)
+        lb.lory_paged_attn(x, cache, cache, torch.zeros(n, 1, dtype=torch.int32, device="cuda"), pos)
+        lb.lory_kv_plan(i32(0), i32(1), i32(0)[None], i32(0), i32(1), 16, i32(0), i32(0, 0), i32(0), torch.zeros(1, dtype=torch.int64, device="cuda"),
+                        i32(0), i32(0))
+        got = {s["name"]: s for s in lb.lory_profile_read()}
+    finally:
+        lb.lory_profile_enable(False)
+    assert set(got) == {"qk_rope", "qk_rope_bwd", "kv_plan", "paged_attn"}
+    assert all(s["launches"] == 1 and s["ms"] > 0 for s in got.values())
+    assert got["qk_rope"]["bytes"] == 4 * n * 2 * H * D * 4 // 2 + 4 * n and got["qk_rope_bwd"]["bytes"] == 3 * 4 * n * 2 * H * D + 4 * n
+
+
 # ---------------------------------------------------------------- under autograd, and all together
 
 def test_autograd_of_norm_and_rotation():
