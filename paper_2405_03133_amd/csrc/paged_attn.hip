@@ -69,6 +69,20 @@ struct Args {
     float scale2;             // scale * log2(e)
 };
 
+// Values are read past the caches where the key-value cache is too large to be found in the memory-side cache (256 MB, of which
+// other layers want their share) when it is read again: from 64 MB on.  us with and without: four rows of 50000 to
+// 131072 tokens 220 / 246, 16 rows of 500 to 3000, 16 heads of 128 36.6 / 42, a ragged batch of 103 MB 28.0 / 30.3; 25 MB that
+// were read just before 10.1 / 9.0.  Keys are not: their lines are read by two instructions each (37.8 there).
+constexpr long kStreamBytes = 64l << 20;
+
+template <bool STREAM, typename V> __device__ __forceinline__ V load_value(const char *p)
+{
+    if constexpr (STREAM)
+        return __builtin_nontemporal_load(reinterpret_cast<const V *>(p));
+    else
+        return *reinterpret_cast<const V *>(p);
+}
+
 template <typename T> constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;   // of a wavefront's step
 template <typename T> constexpr int kTile = kKeys<T> * kWaves;
 
@@ -136,7 +150,7 @@ template <int DP, bool PAD> struct Wave<__hip_bfloat16, DP, PAD> {
             }
         }
     }
-    __device__ static void load_v(Keys &x, const char *base, int row, int D, int i, int c)
+    template <bool STREAM> __device__ static void load_v(Keys &x, const char *base, int row, int D, int i, int c)
     {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -146,14 +160,14 @@ template <int DP, bool PAD> struct Wave<__hip_bfloat16, DP, PAD> {
             for (int m = 0; m < VL; ++m) {
                 if constexpr (VW == 8) {
                     u32x4 y = {0, 0, 0, 0};
-                    if (!PAD || (16 * m + i) * 8 < D) y = *reinterpret_cast<const u32x4 *>(p + m * 256);
+                    if (!PAD || (16 * m + i) * 8 < D) y = load_value<STREAM, u32x4>(p + m * 256);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x.v[j][m][e] = y[e];
                 } else {
-                    uint2 y = {0, 0};
-                    if (!PAD || i * 4 < D) y = *reinterpret_cast<const uint2 *>(p);
-                    x.v[j][m][0] = y.x;
-                    x.v[j][m][1] = y.y;
+                    gemm::u32x2 y = {0, 0};
+                    if (!PAD || i * 4 < D) y = load_value<STREAM, gemm::u32x2>(p);
+                    x.v[j][m][0] = y[0];
+                    x.v[j][m][1] = y[1];
                 }
             }
         }
@@ -237,7 +251,7 @@ template <int DP, bool PAD> struct Wave<float, DP, PAD> {
             if (!PAD || (4 * s + c) * 4 < D) x.k[s] = *reinterpret_cast<const f32x4 *>(p + s * 64);
         }
     }
-    __device__ static void load_v(Keys &x, const char *base, int row, int D, int i, int c)
+    template <bool STREAM> __device__ static void load_v(Keys &x, const char *base, int row, int D, int i, int c)
     {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -246,7 +260,7 @@ template <int DP, bool PAD> struct Wave<float, DP, PAD> {
 #pragma unroll
             for (int m = 0; m < VL; ++m) {
                 if (PAD) x.v[j][m] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (!PAD || (16 * m + i) * 4 < D) x.v[j][m] = *reinterpret_cast<const f32x4 *>(p + m * 256);
+                if (!PAD || (16 * m + i) * 4 < D) x.v[j][m] = load_value<STREAM, f32x4>(p + m * 256);
             }
         }
     }
@@ -302,7 +316,7 @@ template <typename T> __device__ __forceinline__ void write_out(const Args &a, i
 // Tiles t0 .. t1 of head h (a block of up to 16 query heads of a key-value head) of row b, whose length is len: the
 // wavefronts take turns of kKeys keys and join in LDS.  `whole`: the piece is all of the row, its result goes to out; else
 // it goes to slot `slot` of the workspace.
-template <typename T, int DP, bool PAD, int NW>
+template <typename T, int DP, bool PAD, bool STREAM, int NW>
 __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, int h, int t0, int t1, int len, bool whole, int slot)
 {
     using W = Wave<T, DP, PAD>;
@@ -333,7 +347,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
     int row = row_of(at, page);
     if (at < last) {
         W::load_k(x, a.k, max(row, 0), a.D, i, c);
-        W::load_v(x, a.v, max(row, 0), a.D, i, c);
+        W::template load_v<STREAM>(x, a.v, max(row, 0), a.D, i, c);
     }
     for (; at < last; at += STEP) {
 #pragma clang fp contract(off)
@@ -375,7 +389,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             l += s[n];
         }
         w.add(x, s);
-        if (more) W::load_v(x, a.v, max(row, 0), a.D, i, c);
+        if (more) W::template load_v<STREAM>(x, a.v, max(row, 0), a.D, i, c);
     }
     l = xor_sum(l);
 
@@ -418,19 +432,19 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
 
 // A row's units in equal ranges, a workgroup each: grid (ranges, heads, rows).  One range: all of the row, and nothing is left
 // to join.
-template <typename T, int DP, bool PAD, int NW> __global__ __launch_bounds__(64 * NW) void paged_attn_rows_kernel(Args a)
+template <typename T, int DP, bool PAD, bool STREAM, int NW> __global__ __launch_bounds__(64 * NW) void paged_attn_rows_kernel(Args a)
 {
     __shared__ Shared<DP, NW> sh;
     const int s = blockIdx.x, S = gridDim.x, h = blockIdx.y;
     for (int b = blockIdx.z; b < a.rows; b += gridDim.z) {
         const int len = length_of(a, b), units = units_of<T>(len);
         const int t0 = S == 1 ? 0 : (int)paged::range_begin(s, units, S), t1 = S == 1 ? units : (int)paged::range_begin(s + 1, units, S);
-        if (t0 < t1) piece<T, DP, PAD, NW>(a, sh, b, h, t0, t1, len, t0 == 0 && t1 == units, (int)(((unsigned)b * gridDim.y + h) * S + s));
+        if (t0 < t1) piece<T, DP, PAD, STREAM, NW>(a, sh, b, h, t0, t1, len, t0 == 0 && t1 == units, (int)(((unsigned)b * gridDim.y + h) * S + s));
     }
 }
 
 // Equal ranges of the units of all rows and heads.
-template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Args a)
+template <typename T, int DP, bool PAD, bool STREAM> __global__ __launch_bounds__(kThreads) void paged_attn_kernel(Args a)
 {
     __shared__ Shared<DP, kWaves> sh;
     __shared__ int wsum[kWaves];
@@ -480,7 +494,7 @@ template <typename T, int DP, bool PAD> __global__ __launch_bounds__(kThreads) v
 
     while (u < end) {
         const int stop = (int)(end - u < units - tile ? tile + (end - u) : units);
-        piece<T, DP, PAD, kWaves>(a, sh, b, h, tile, stop, len, tile == 0 && stop == units, 2 * blockIdx.x + (tile == 0 ? 1 : 0));
+        piece<T, DP, PAD, STREAM, kWaves>(a, sh, b, h, tile, stop, len, tile == 0 && stop == units, 2 * blockIdx.x + (tile == 0 ? 1 : 0));
         u += stop - tile;
         tile = 0;
         if (stop == units && ++h == heads && u < end) {
@@ -583,7 +597,7 @@ Plan plan(const lory_paged_shape &s)
     return {0, 2 * kCUs * resident(s.head_dim)};
 }
 
-template <typename T, int DP, bool PAD> void launch3(const Args &a, const Plan &p, hipStream_t st)
+template <typename T, int DP, bool PAD, bool STREAM> void launch4(const Args &a, const Plan &p, hipStream_t st)
 {
     const dim3 join(a.Hkv * a.tiles, a.rows < 32768 ? a.rows : 32768);
     Args g = a;
@@ -594,15 +608,23 @@ template <typename T, int DP, bool PAD> void launch3(const Args &a, const Plan &
         bool wide = false;
         if constexpr (DP <= 128) {   // eight wavefronts of the widest heads would spill
             wide = all <= 256;
-            if (wide) hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 8>), grid, dim3(512), 0, st, g);
+            if (wide) hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, STREAM, 8>), grid, dim3(512), 0, st, g);
         }
-        if (!wide) hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, 4>), grid, dim3(256), 0, st, g);
+        if (!wide) hipLaunchKernelGGL((paged_attn_rows_kernel<T, DP, PAD, STREAM, 4>), grid, dim3(256), 0, st, g);
         if (p.ranges > 1) hipLaunchKernelGGL((paged_attn_join_kernel<T, true>), join, dim3(kJoinThreads), 0, st, g);
         return;
     }
     g.groups = kCUs * resident(DP);
-    hipLaunchKernelGGL((paged_attn_kernel<T, DP, PAD>), dim3(g.groups), dim3(kThreads), 0, st, g);
+    hipLaunchKernelGGL((paged_attn_kernel<T, DP, PAD, STREAM>), dim3(g.groups), dim3(kThreads), 0, st, g);
     hipLaunchKernelGGL((paged_attn_join_kernel<T, false>), join, dim3(kJoinThreads), 0, st, g);
+}
+
+template <typename T, int DP, bool PAD> void launch3(const Args &a, const Plan &p, hipStream_t st)
+{
+    if (2 * (long)a.pages * a.Hkv * a.page * a.D * (long)sizeof(T) > kStreamBytes)
+        launch4<T, DP, PAD, true>(a, p, st);
+    else
+        launch4<T, DP, PAD, false>(a, p, st);
 }
 
 template <typename T, int DP> void launch2(const Args &a, const Plan &p, hipStream_t st)

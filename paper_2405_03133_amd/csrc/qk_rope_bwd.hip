@@ -31,7 +31,8 @@ struct Args {
 
 template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds__(64 * kWaves, 4) void qk_rope_bwd_kernel(Args a)
 {
-    constexpr int VEC = 16 / sizeof(T), HPW = 64 / LPH, U = 2;
+    constexpr int VEC = 16 / sizeof(T), HPW = 64 / LPH;
+    constexpr int U = sizeof(T) == 4 ? 4 : 2;   // groups in flight, what the registers allow
     __shared__ float2 table[kWaves][kMaxPairs];
     __shared__ float sums[kWaves][2 * LPH * VEC];
     const int lane = threadIdx.x & 63, wave = wave_index();
