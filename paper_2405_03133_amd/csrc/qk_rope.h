@@ -32,11 +32,16 @@ __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstl
 typedef uint32_t Chunk __attribute__((ext_vector_type(4)));
 
 // Results are written past the caches (their readers are other launches, mostly on other XCDs): prompts of 12001 tokens into
-// the cache 38.4 -> 28.0 us, 16384 tokens of 32 heads of 128 55.5 -> 52.2.  The gradient also reads past them (99 -> 83 us
-// there; the forward gets slower: 28 -> 34 us into the cache).
+// the cache 38.4 -> 28.0 us, 16384 tokens of 32 heads of 128 55.5 -> 52.2.  Loads past them: the gradient's (99 -> 83 us
+// there when it came in, 84 -> 80 now; 74 MB of fp32 18.5 -> 19.0) and those of large forward calls.
 __device__ __forceinline__ void store_once(char *p, Chunk v) { __builtin_nontemporal_store(v, reinterpret_cast<Chunk *>(p)); }
-
-__device__ __forceinline__ Chunk load_once(const char *p) { return __builtin_nontemporal_load(reinterpret_cast<const Chunk *>(p)); }
+template <bool STREAM> __device__ __forceinline__ Chunk load(const char *p)
+{
+    if constexpr (STREAM)
+        return __builtin_nontemporal_load(reinterpret_cast<const Chunk *>(p));
+    else
+        return *reinterpret_cast<const Chunk *>(p);
+}
 
 template <typename T> __device__ __forceinline__ void widen(Chunk r, float (&v)[16 / sizeof(T)])
 {

@@ -32,7 +32,8 @@ struct Args {
     float eps;
 };
 
-template <typename T, int LPH, bool INTER, bool STORE> __global__ __launch_bounds__(64 * kWaves) void qk_rope_kernel(Args a)
+// STREAM: the heads are read past the caches.
+template <typename T, int LPH, bool INTER, bool STORE, bool STREAM> __global__ __launch_bounds__(64 * kWaves) void qk_rope_kernel(Args a)
 {
     constexpr int VEC = 16 / sizeof(T), HPW = 64 / LPH;   // heads of a group: one load of the wavefront
     constexpr int U = 4;                                  // groups in flight
@@ -91,7 +92,7 @@ template <typename T, int LPH, bool INTER, bool STORE> __global__ __launch_bound
                     const int h = (g + u) * HPW + l.sub;
                     raw[u] = Chunk{0, 0, 0, 0};
                     if (g + u < hi && h < H && l.on)
-                        raw[u] = *reinterpret_cast<const Chunk *>(src + h * src_head + l.chunk * 16);
+                        raw[u] = load<STREAM>(src + h * src_head + l.chunk * 16);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -126,10 +127,14 @@ template <typename T, int LPH, bool INTER, bool STORE> __global__ __launch_bound
         for (int g = lo; g < g1 - gq - gk; ++g) {
             const int h = g * HPW + l.sub;
             if (h < a.Hkv)
-                store_once(vrow + h * khead + l.chunk * 16, *reinterpret_cast<const Chunk *>(src + h * a.v.head));
+                store_once(vrow + h * khead + l.chunk * 16, load<STREAM>(src + h * a.v.head));
         }
     }
 }
+
+// Heads of more than 128 MB are read past the caches: less is what the 256 MB memory-side cache may still hold from the
+// projection (us with and without: 134 MB read 49.7 / 52.3, 165 MB 45.7 / 46.7; 74 MB 30.7 / 26.2, 21 MB 13.9 / 11.3, just written).
+constexpr long kStreamBytes = 128l << 20;
 
 template <typename T, int LPH, bool STORE> void launch2(const Args &a, bool inter, hipStream_t st)
 {
@@ -140,11 +145,16 @@ template <typename T, int LPH, bool STORE> void launch2(const Args &a, bool inte
     // so, and more wavefronts cost larger calls the angles again: 4093 fp32 tokens 15.7 us against 11.3)
     int ny = (1024 + blocks - 1) / blocks;
     if (ny > groups) ny = groups;
-    const dim3 grid(blocks, ny);
-    if (inter)
-        hipLaunchKernelGGL((qk_rope_kernel<T, LPH, true, STORE>), grid, dim3(64 * kWaves), 0, st, a);
+    const dim3 grid(blocks, ny), block(64 * kWaves);
+    const bool stream = (long)a.tokens * (a.Hq + (STORE ? 2 : 1) * a.Hkv) * a.D * (long)sizeof(T) > kStreamBytes;
+    if (inter && stream)
+        hipLaunchKernelGGL((qk_rope_kernel<T, LPH, true, STORE, true>), grid, block, 0, st, a);
+    else if (inter)
+        hipLaunchKernelGGL((qk_rope_kernel<T, LPH, true, STORE, false>), grid, block, 0, st, a);
+    else if (stream)
+        hipLaunchKernelGGL((qk_rope_kernel<T, LPH, false, STORE, true>), grid, block, 0, st, a);
     else
-        hipLaunchKernelGGL((qk_rope_kernel<T, LPH, false, STORE>), grid, dim3(64 * kWaves), 0, st, a);
+        hipLaunchKernelGGL((qk_rope_kernel<T, LPH, false, STORE, false>), grid, block, 0, st, a);
 }
 
 template <typename T, bool STORE> void launch1(const Args &a, bool inter, hipStream_t st)

@@ -66,8 +66,8 @@ template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds
                     const int h = (g + u) * HPW + l.sub;
                     rx[u] = rg[u] = Chunk{0, 0, 0, 0};
                     if (g + u < hi && h < H && l.on) {
-                        if constexpr (NORM) rx[u] = load_once(src + h * src_head + l.chunk * 16);
-                        rg[u] = load_once(grad + h * grad_head + l.chunk * 16);
+                        if constexpr (NORM) rx[u] = load<true>(src + h * src_head + l.chunk * 16);
+                        rg[u] = load<true>(grad + h * grad_head + l.chunk * 16);
                     }
                 }
 #pragma unroll
