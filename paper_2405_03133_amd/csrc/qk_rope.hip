@@ -132,9 +132,9 @@ template <typename T, int LPH, bool INTER, bool STORE, bool STREAM> __global__ _
     }
 }
 
-// Heads of more than 128 MB are read past the caches: less is what the 256 MB memory-side cache may still hold from the
+// Heads of more than 96 MB are read past the caches: less is what the 256 MB memory-side cache may still hold from the
 // projection (us with and without: 134 MB read 49.7 / 52.3, 165 MB 45.7 / 46.7; 74 MB 30.7 / 26.2, 21 MB 13.9 / 11.3, just written).
-constexpr long kStreamBytes = 128l << 20;
+constexpr long kStreamBytes = 96l << 20;
 
 template <typename T, int LPH, bool STORE> void launch2(const Args &a, bool inter, hipStream_t st)
 {

@@ -110,6 +110,25 @@ def test_rope(n, Hq, Hkv, D, rot, inter, dtype):
         assert torch.equal(y[..., rot:], x[..., rot:])
 
 
+@pytest.mark.parametrize("n,Hq,Hkv,D,rot,inter,dtype", [(7000, 24, 8, 128, 128, False, "f32"), (13001, 20, 5, 256, 64, True, "bf16")])
+def test_rope_of_more_than_100_megabytes(n, Hq, Hkv, D, rot, inter, dtype):
+    """Large calls are read another way; the store too."""
+    g, t = gen(n), T[dtype]
+    q, k, v = rnd(g, n, Hq, D, dtype=t), rnd(g, n, Hkv, D, dtype=t), rnd(g, n, Hkv, D, dtype=t)
+    wq, wk = (1 + 0.3 * rnd(g, D)).to(t), (1 + 0.3 * rnd(g, D)).to(t)
+    pos, freq = torch.randint(0, 5000, (n,), device="cuda", dtype=torch.int32), freqs(rot)
+    w = dict(wq=wq, wk=wk, eps=EPS, interleaved=inter)
+    yq, yk = lb.lory_qk_rope(q, k, pos, freq, **w)
+    for name, y, x, wx in (("q", yq, q, wq), ("k", yk, k, wk)):
+        ref, size = rope_ref(x, wx, pos, freq, inter)
+        within(f"{name} {n}x{x.shape[1]}x{D}", y, ref, ROPE * size, t)
+    page = 16
+    kc, vc = (torch.zeros(-(-n // page), Hkv, page, D, device="cuda", dtype=t) for _ in range(2))
+    slots = torch.randperm(kc.shape[0] * page, device="cuda")[:n]
+    assert torch.equal(lb.lory_qk_rope_cache(q, k, v, pos, freq, kc, vc, slots, **w), yq)
+    assert torch.equal(kc[slots // page, :, slots % page], yk) and torch.equal(vc[slots // page, :, slots % page], v)
+
+
 def test_rope_strides_far_positions_and_in_place():
     g = gen(3)
     n, Hq, Hkv, D, rot = 37, 6, 2, 128, 128
@@ -390,7 +409,7 @@ def test_plan_without_rows():
 
 # ---------------------------------------------------------------- attention
 
-def paged_case(seed, lens, Hq, Hkv, D, page, dtype, width=None, sigma=2.0):
+def paged_case(seed, lens, Hq, Hkv, D, page, dtype, width=None, sigma=2.0, least_bytes=0):
     """q, caches whose unused places hold NaN and infinities, a table whose unused entries are no pages."""
     g = gen(seed)
     t = T[dtype]
@@ -398,6 +417,8 @@ def paged_case(seed, lens, Hq, Hkv, D, page, dtype, width=None, sigma=2.0):
     blocks = -(-lens // page)
     W = width or max(1, int(blocks.max(initial=0)))
     total = int(blocks.sum()) + 3
+    while 2 * total * Hkv * page * D * t.itemsize <= least_bytes:
+        total *= 2
     perm = np.random.RandomState(seed).permutation(total)
     table = np.random.RandomState(seed + 1).choice([-1, total, 2 ** 31 - 1, -2 ** 31, 10 ** 6], size=(len(lens), W))
     table[np.arange(W)[None] < blocks[:, None]] = perm[:blocks.sum()]
@@ -495,6 +516,49 @@ def test_attention_many_rows(B):
     lens = np.random.RandomState(B).randint(0, 90, B)
     case = paged_case(B, lens, 4, 2, 64, 16, "bf16")
     check_attention(f"{B} rows", *attend(case), *case)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,Hq,Hkv,D,page", [([0, 1, 31, 300, 65], 8, 2, 64, 16), ([5000, 3, 129], 12, 4, 128, 16),
+                                                ([700, 64], 3, 1, 40, 8), ([333, 4000], 20, 4, 80, 24), ([77, 2100], 6, 2, 256, 16),
+                                                ([90, 500], 17, 1, 200, 32)])
+def test_attention_of_a_large_cache(lens, Hq, Hkv, D, page, dtype):
+    """Caches of more than 64 MB are read another way."""
+    case = paged_case(len(lens) + D, lens, Hq, Hkv, D, page, dtype, least_bytes=64 << 20)
+    check_attention(f"large cache {lens[:3]} {Hq}/{Hkv}x{D}", *attend(case), *case)
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_attention_of_more_rows_than_a_grid_dimension(wide):
+    """70000 rows of up to four tokens, in one launch or (a table that allows long rows, and three long ones) in ranges."""
+    B, D, page, W = 70000, 8, 4096 if wide else 4, 8 if wide else 1
+    g = gen(3)
+    lens = torch.randint(0, 5, (B,), generator=g, device="cuda", dtype=torch.int32)
+    pages = 24 if wide else 1000
+    k, v = rnd(g, pages, 1, page, D), rnd(g, pages, 1, page, D)
+    table = torch.randint(0, pages, (B, W), generator=g, device="cuda", dtype=torch.int32)
+    q = rnd(g, B, 1, D)
+    long = {17: 9000, 40000: 32768, B - 1: 4097} if wide else {}
+    for b, n in long.items():
+        lens[b] = n
+    lse = torch.empty(B, 1, device="cuda")
+    out = lb.lory_paged_attn(q, k, v, table, lens, lse=lse)
+    short = torch.ones(B, dtype=torch.bool, device="cuda")
+    short[list(long)] = False
+    here = torch.arange(4, device="cuda") < lens[:, None]
+    K, V = (x[table[:, 0].long(), 0, :4].double() for x in (k, v))
+    z = (K * q.double()).sum(-1) * D ** -0.5
+    z = torch.where(here, z, float("-inf"))
+    p = torch.softmax(z, -1).nan_to_num(0.0)
+    # as in check_attention: scores of D terms, one chain of additions
+    dz = (K.abs() * q.double().abs()).sum(-1).amax(-1) * D ** -0.5 * (D + 6) * E32
+    rel = (2 * dz + (4 + 2 * 65) * E32)[:, None]
+    ref, bound = (p[..., None] * V).sum(1), rel * (p[..., None] * V.abs()).sum(1)
+    within("many rows", out[short, 0], ref[short], bound[short], torch.float32)
+    rl = torch.logsumexp(z, -1)
+    within("many rows lse", lse[short, 0], rl[short], (dz + 80 * E32 + 4 * E32 * rl.abs().nan_to_num(0.0, 0.0))[short])
+    for b in long:
+        check_attention(f"long row {b}", out[b:b + 1], lse[b:b + 1], q[b:b + 1], k, v, table[b:b + 1], lens[b:b + 1])
 
 
 def test_attention_strides_scale_and_in_place():
