@@ -6,7 +6,7 @@
 // binary search over the sums of chunks of rows in LDS and a walk inside the chunk.  Pages that come back are never read from
 // where another workgroup may just write them: place j of the grown stack is free[j] below the old top and the
 // page table's own entry above it, entries that no workgroup changes.  Tokens and pages are one list, a thread each: one
-// loop after the other took 9.0 us where this takes 6.8 (1000 rows, 88000 new tokens).  64 rows with a token each: 3.9 us, a
+// loop after the other took 9.0 us where this takes 6.7 (1000 rows, 88000 new tokens).  64 rows with a token each: 3.8 us, a
 // launch that does nothing 1.8.
 #include "lory_internal.h"
 

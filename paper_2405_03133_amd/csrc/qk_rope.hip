@@ -8,8 +8,8 @@
 // Four groups of heads are loaded at a time; two or eight were slower (16384 tokens of 32 heads of 128, bf16: 55.4 and 54.9 us
 // against 52.1), and so was loading queries, keys and values before the angles are formed (57.4: the registers for it cost two
 // of six wavefronts per SIMD).
-// Measured: those 16384 tokens 50.6 us, 5.3 TB/s; prompts of 12001 tokens (16 + 4 heads) into the cache 25.7 us, 5.7 TB/s; 4093
-// fp32 tokens (16 heads of 80, 20 of 32 lanes in use) 11.1 us, 3.8 TB/s; 48 tokens into the cache 4.2 us, of which a launch
+// Measured: those 16384 tokens 48.5 us, 5.5 TB/s; prompts of 12001 tokens (16 + 4 heads) into the cache 25.8 us, 5.7 TB/s; 4093
+// fp32 tokens (16 heads of 80, 20 of 32 lanes in use) 11.0 us, 3.8 TB/s; 48 tokens into the cache 4.2 us, of which a launch
 // that does nothing takes 1.8.  HBM traffic is that of the heads alone (134.9 + 134.2 MB of 268.5).
 #include "qk_rope.h"
 
