@@ -73,6 +73,7 @@ class _QkRope(torch.autograd.Function):
         return lb.lory_qk_rope(q, k, pos, freq, wq=wq, wk=wk, eps=eps, interleaved=interleaved)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, dq_out, dk_out):
         q, k, pos, freq, wq, wk = ctx.saved_tensors
         dq, dk, dwq, dwk = lb.lory_qk_rope_bwd(q, k, dq_out.contiguous(), dk_out.contiguous(), pos, freq, wq, wk, ctx.eps,

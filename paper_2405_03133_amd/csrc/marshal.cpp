@@ -195,6 +195,10 @@ PyObject *result(int status, std::initializer_list<at::Tensor> out)
         PyObject *o;
         if (x.defined()) {
             o = THPVariable_Wrap(x);
+            if (!o) {
+                Py_DECREF(t);
+                throw Raised();
+            }
         } else {
             Py_INCREF(Py_None);
             o = Py_None;

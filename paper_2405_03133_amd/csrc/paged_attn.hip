@@ -41,7 +41,7 @@ using gemm::bf16x8;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256, kWaves = 4, kJoinThreads = 512;
+constexpr int kThreads = 256, kWaves = 4, kJoinThreads = 256;
 constexpr int kCUs = 256;
 // Workgroups of four wavefronts that the registers let a CU hold (heads of up to 64, 128, 256): 100 rows of 100 to 4000 tokens,
 // 8 heads of 64, in 512 ranges 58.8 us, in 768 52.2.
@@ -506,12 +506,13 @@ template <typename T, int DP, bool PAD, bool STREAM> __global__ __launch_bounds_
     }
 }
 
-// Joins the pieces of one row's head, grid (heads, rows): every thread takes two dims of one query over a share of the pieces,
+// Joins the pieces of one row's head, grid (heads, rows): every thread takes four dims of one query over a share of the pieces,
 // maximum, sum and output at once (one read of memory behind the row's place), and the shares are added in order.  BY_ROW:
 // the pieces are those of paged_attn_rows_kernel.
 template <typename T, bool BY_ROW> __global__ __launch_bounds__(kJoinThreads) void paged_attn_join_kernel(Args a)
 {
-    __shared__ f32x4 scratch[kJoinThreads];
+    __shared__ f32x4 so[kJoinThreads];
+    __shared__ float2 sml[kJoinThreads];
     const int h = blockIdx.x, heads = gridDim.x, tid = threadIdx.x;
     for (int b = blockIdx.y; b < a.rows; b += gridDim.y) {
         const int units = BY_ROW ? units_of<T>(length_of(a, b)) : a.starts[b + 1] - a.starts[b];
@@ -529,42 +530,54 @@ template <typename T, bool BY_ROW> __global__ __launch_bounds__(kJoinThreads) vo
         const int kvh = a.tiles == 1 ? h : h / a.tiles, first = kvh * a.group + (h - kvh * a.tiles) * 16;
         const int nq = min(16, (kvh + 1) * a.group - first);
 
-        const int pairs = a.D / 2, all = nq * pairs;
+        const int quads = a.D / 4, all = nq * quads;
         int per = 16;   // threads that share a piece
         while (per < all && per < kJoinThreads) per <<= 1;
         const int shares = kJoinThreads / per, share = tid / per;
         for (int x0 = 0; x0 < all; x0 += per) {
             const int x = x0 + tid % per;
             const bool on = x < all;
-            const int j = on ? x / pairs : 0, d = on ? x - j * pairs : 0;
-            float M = -INFINITY, L = 0.f, O0 = 0.f, O1 = 0.f;
-            auto take = [&](float m, float l, float o0, float o1) {
+            const int j = on ? x / quads : 0, d = on ? x - j * quads : 0;
+            float M = -INFINITY, L = 0.f;
+            f32x4 O = {0.f, 0.f, 0.f, 0.f};
+            auto take = [&](float m, float l, f32x4 o) {
                 const float M1 = fmaxf(M, m), ref = M1 == -INFINITY ? 0.f : M1;
                 const float f = __builtin_amdgcn_exp2f(M - ref), g = __builtin_amdgcn_exp2f(m - ref);
                 L = L * f + l * g;
-                O0 = O0 * f + o0 * g;
-                O1 = O1 * f + o1 * g;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[e] = O[e] * f + o[e] * g;
                 M = M1;
             };
-            if (on) {
-#pragma unroll 8
-                for (int p = share; p < parts; p += shares) {
-                    const long at = (long)slot_of(p) * a.part_rows + j;
-                    const float2 ml = a.part_ml[at], o = a.part_o[at * pairs + d];
-                    take(ml.x, ml.y, o.x, o.y);
+            // eight pieces at a time, all under way at once; where there are fewer, the last ones are empty
+            for (int p0 = share; on && p0 < parts; p0 += 8 * shares) {
+                float2 ml[8];
+                f32x4 o[8];
+#pragma unroll
+                for (int n = 0; n < 8; ++n) {
+                    ml[n] = make_float2(-INFINITY, 0.f);
+                    o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    if (p0 + n * shares < parts) {
+                        const long at = (long)slot_of(p0 + n * shares) * a.part_rows + j;
+                        ml[n] = a.part_ml[at];
+                        o[n] = *reinterpret_cast<const f32x4 *>(a.part_o + at * 2 * quads + 2 * d);
+                    }
                 }
+#pragma unroll
+                for (int n = 0; n < 8; ++n) take(ml[n].x, ml[n].y, o[n]);
             }
             if (shares > 1) {
-                scratch[tid] = f32x4{M, L, O0, O1};
+                so[tid] = O;
+                sml[tid] = make_float2(M, L);
                 __syncthreads();
                 if (share == 0)
-                    for (int n = 1; n < shares; ++n) {
-                        const f32x4 v = scratch[n * per + tid];
-                        take(v[0], v[1], v[2], v[3]);
-                    }
+                    for (int n = 1; n < shares; ++n) take(sml[n * per + tid].x, sml[n * per + tid].y, so[n * per + tid]);
                 __syncthreads();
             }
-            if (share == 0 && on) write_out<T>(a, b, first + j, 2 * d, M == -INFINITY ? 0.f : M, L, O0, O1);
+            if (share == 0 && on) {
+                const float ref = M == -INFINITY ? 0.f : M;
+                write_out<T>(a, b, first + j, 4 * d, ref, L, O[0], O[1]);
+                write_out<T>(a, b, first + j, 4 * d + 2, ref, L, O[2], O[3]);
+            }
         }
     }
 }

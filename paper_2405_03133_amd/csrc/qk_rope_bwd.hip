@@ -136,9 +136,14 @@ __global__ __launch_bounds__(1024) void qk_rope_dw_kernel(const float *part, int
     __shared__ float sums[64][kDwColumns];
     const int c = threadIdx.x % kDwColumns, g = threadIdx.x / kDwColumns;
     const int col = blockIdx.x * kDwColumns + c;   // below 2 D, which is a multiple of 16
-    float v = 0.f;
-#pragma unroll 8
-    for (int r = g; r < rows; r += 64) v += part[(size_t)r * 2 * D + col];
+    float x[kMaxBlocks / 64], v = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMaxBlocks / 64; ++i) {   // all under way at once
+        x[i] = 0.f;
+        if (g + 64 * i < rows) x[i] = part[(size_t)(g + 64 * i) * 2 * D + col];
+    }
+#pragma unroll
+    for (int i = 0; i < kMaxBlocks / 64; ++i) v += x[i];
     sums[g][c] = v;
     __syncthreads();
     if (threadIdx.x >= 64) return;
