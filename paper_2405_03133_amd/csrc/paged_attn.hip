@@ -21,8 +21,8 @@
 //
 // Pages: the lane that owns a key looks its page up two steps ahead; the others fetch the row by a lane permute.
 //
-// Measured: four rows of 50000 to 131072 tokens, 32 query heads on 8, heads of 128, bf16: 215 us + 6.7 for the join, 6.6 TB/s
-// (a pass that only reads reaches 6.7); 48 rows of 1 to 9000 tokens 21.6 + 5.9 us, 4.8 TB/s; HBM traffic is the cache's
+// Measured: four rows of 50000 to 131072 tokens, 32 query heads on 8, heads of 128, bf16: 216 us + 5.8 for the join, 6.6 TB/s
+// (a pass that only reads reaches 6.7); 48 rows of 1 to 9000 tokens 22.5 + 5.0 us, 4.6 TB/s; HBM traffic is the cache's
 // bytes and 1 MB of pieces.  One CU takes in about 60 bytes per ns however many loads are under way (a second step in flight,
 // 16 wavefronts instead of eight or steps of 16 keys change nothing), so a short row costs 4 us and its bytes at that
 // rate.  Joining in the workgroup that finishes last instead of a second launch was tried: with fences between the XCDs

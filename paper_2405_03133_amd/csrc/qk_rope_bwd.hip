@@ -8,7 +8,7 @@
 // 128 registers, four wavefronts per SIMD and 1024 workgroups, all resident at once: with 141 registers a quarter of them
 // waited for a second round (99 us against 79 for 16384 tokens of 32 heads of 128, bf16).  Workgroups of eight or 16 wavefronts leave
 // fewer rows to add but measured the same or slower (79.6, 86).
-// Measured: those 16384 tokens 72.4 us, 5.6 TB/s, and 4.5 us for the rows; 2999 fp32 tokens of 24 + 8 heads of 64 16.0 + 3.9 us.
+// Measured: those 16384 tokens 73.4 us, 5.5 TB/s, and 4.6 us for the rows; 2999 fp32 tokens of 24 + 8 heads of 64 16.6 + 3.9 us.
 #include "qk_rope.h"
 
 namespace lory {
@@ -128,7 +128,7 @@ template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds
 }
 
 // dw from the rows of partial sums, 16 columns a workgroup: a thread takes every 64th row of its column, the 64 sums of a column
-// are added in order, a quarter per lane, and the quarters last.  1024 rows of 2 x 128: 4.5 us, a launch and three latencies.
+// are added in order, a quarter per lane, and the quarters last.  1024 rows of 2 x 128: 4.6 us, a launch and three latencies.
 constexpr int kDwColumns = 16;
 
 __global__ __launch_bounds__(1024) void qk_rope_dw_kernel(const float *part, int rows, int D, float *dwq, float *dwk)
