@@ -339,7 +339,8 @@ int lory_merged_ffn_bwd(const lory_shape *shape, const void *X, const float *w,
  * (tokens, rows, room) may be 0, and with 0 of them the pointers that hold them
  * may be NULL; integer and double arrays are aligned to their element only; heads are
  * strided.  `lory_heads` is a [tokens, heads, head_dim] tensor whose last index
- * is contiguous; token and head are its strides in elements, >= 0.  data is
+ * is contiguous; token and head are its strides in elements, 0 .. 2^36 (so is
+ * table_row below, at least width).  data is
  * 16-byte aligned and both strides are multiples of 16 bytes (slices of one
  * [tokens, (q_heads + 2 kv_heads) * head_dim] product are passed as they lie;
  * the stride of a dimension of one entry is not used).  Inputs are read only.

@@ -8,6 +8,8 @@ namespace {
 
 bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+constexpr int64_t kMaxStride = (int64_t)1 << 36;   // elements; times any number of rows it stays far inside 64 bits
+
 // esize of a dtype, 0: unknown
 int esize_of(int dtype) { return dtype == LORY_F32 ? 4 : dtype == LORY_BF16 ? 2 : 0; }
 
@@ -22,7 +24,7 @@ int check_heads_dims(int q_heads, int kv_heads, int head_dim)
 int check_heads(const lory_heads *h, long tokens, long heads, int esize)
 {
     if (!h || (tokens > 0 && !h->data)) return LORY_ERR_NULL;
-    if (h->token < 0 || h->head < 0) return LORY_ERR_SHAPE;
+    if (h->token < 0 || h->head < 0 || h->token > kMaxStride || h->head > kMaxStride) return LORY_ERR_SHAPE;
     const int n = 16 / esize;
     if (!aligned(h->data, 16) || (tokens > 1 && h->token % n != 0) || (heads > 1 && h->head % n != 0)) return LORY_ERR_ALIGN;
     return LORY_OK;
@@ -87,7 +89,8 @@ int check_paged(const lory_paged_shape *s)
     const int rc = check_heads_dims(s->q_heads, s->kv_heads, s->head_dim);
     if (rc != LORY_OK) return rc;
     if (s->q_heads % s->kv_heads != 0) return LORY_ERR_SHAPE;
-    if (s->pages <= 0 || s->page <= 0 || s->width <= 0 || s->table_row < s->width) return LORY_ERR_SHAPE;
+    if (s->pages <= 0 || s->page <= 0 || s->width <= 0 || s->table_row < s->width || s->table_row > kMaxStride)
+        return LORY_ERR_SHAPE;
     if ((long)s->width * s->page > (1l << 30)) return LORY_ERR_SHAPE;
     // the kernel counts the row's blocks of 64 keys in 32 bits
     if (s->rows * ((long)s->width * s->page / 64 + 1) >= (1l << 31)) return LORY_ERR_SHAPE;
@@ -176,7 +179,7 @@ int lory_kv_plan(const lory_plan_shape *shape, const int32_t *lens, const int32_
     if (!shape) return LORY_ERR_NULL;
     const lory_plan_shape &s = *shape;
     if (s.rows < 0 || s.rows > (1 << 20) || s.room < 0 || s.width <= 0 || s.page <= 0 || s.free_size <= 0 ||
-        s.table_row < s.width || (long)s.width * s.page >= (1l << 31))
+        s.table_row < s.width || s.table_row > kMaxStride || (long)s.width * s.page >= (1l << 31))
         return LORY_ERR_SHAPE;
     if (!free || !count || !cu || !count_new || !status || (s.rows > 0 && (!lens || !add || !table || !lens_new)) ||
         (s.room > 0 && (!positions || !slots)))
