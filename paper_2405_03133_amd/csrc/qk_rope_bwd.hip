@@ -4,7 +4,7 @@
 //   dx = r g w - x r^3 / D * sum(g w x),   dw += g x r,
 // so both sums of a head (x^2 and g w x) come from the same registers.  Wavefronts walk over tokens and keep dw of their
 // chunk in registers; every workgroup adds its wavefronts in LDS and leaves one row of partial sums, and a second
-// launch adds the rows in order: the same bits on every run.
+// launch adds the rows in order: the same bits on every run.  A few tokens take one workgroup, and that launch only (kAlone).
 // 128 registers, four wavefronts per SIMD and 1024 workgroups, all resident at once: with 141 registers a quarter of them
 // waited for a second round (99 us against 79 for 16384 tokens of 32 heads of 128, bf16).  Workgroups of eight or 16 wavefronts leave
 // fewer rows to add but measured the same or slower (79.6, 86).
@@ -18,6 +18,12 @@ namespace {
 using namespace rope;
 
 constexpr int kMaxBlocks = 1024;   // rows of partial sums
+// A few tokens with norms take one workgroup of 16 wavefronts, which writes dw itself, and no second launch: at most 16 tokens, a
+// wavefront each, and kAloneBytes of heads and gradients read and written, as one CU moves about 60 bytes per ns.  Called eagerly
+// and from a graph, one launch against two: bf16 15 KB 7.1 and 4.7 us against 9.7 and 6.5, 60 KB 7.1 and 6.5 against 9.8 and 6.5,
+// 120 KB 7.8 and 7.7 against 9.8 and 6.6, 240 KB 9.8 and 9.8 against 9.8 and 6.6.
+constexpr int kAlone = 16;
+constexpr long kAloneBytes = 128 << 10;
 
 struct Args {
     Heads q, k, dyq, dyk, dq, dk;
@@ -25,16 +31,18 @@ struct Args {
     const double *freq;
     const void *wq, *wk;
     float *part;   // [blocks][2][D]
+    float *dwq, *dwk;
     int tokens, shares, Hq, Hkv, D, rot;
     float eps;
 };
 
-template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds__(64 * kWaves, 4) void qk_rope_bwd_kernel(Args a)
+// WAVES wavefronts a workgroup: kWaves, or kAlone for a launch of one workgroup, which writes dw itself.
+template <typename T, int LPH, bool INTER, bool NORM, int WAVES> __global__ __launch_bounds__(64 * WAVES, 4) void qk_rope_bwd_kernel(Args a)
 {
     constexpr int VEC = 16 / sizeof(T), HPW = 64 / LPH;
     constexpr int U = sizeof(T) == 4 ? 4 : 2;   // groups in flight, what the registers allow
-    __shared__ float2 table[kWaves][kMaxPairs];
-    __shared__ float sums[kWaves][2 * LPH * VEC];
+    __shared__ float2 table[WAVES][kMaxPairs];
+    __shared__ float sums[WAVES][2 * LPH * VEC];
     const int lane = threadIdx.x & 63, wave = wave_index();
     const Lane l = lane_of<T, LPH, INTER>(lane, a.D, a.rot);
     const int gq = (a.Hq + HPW - 1) / HPW, gk = (a.Hkv + HPW - 1) / HPW, groups = gq + gk;
@@ -47,7 +55,7 @@ template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds
 
     // an item is a share of a token's heads
     const long items = (long)a.tokens * a.shares;
-    for (long item = (long)blockIdx.x * kWaves + wave; item < items; item += (long)gridDim.x * kWaves) {
+    for (long item = (long)blockIdx.x * WAVES + wave; item < items; item += (long)gridDim.x * WAVES) {
         const int t = (int)(item / a.shares), share = (int)(item - (long)t * a.shares);
         const int g0 = share * groups / a.shares, g1 = (share + 1) * groups / a.shares;
         const double pos = a.pos[t];
@@ -120,9 +128,15 @@ template <typename T, int LPH, bool INTER, bool NORM> __global__ __launch_bounds
         }
         __syncthreads();
         float *dst = a.part + (size_t)blockIdx.x * 2 * a.D;
-        for (int i = threadIdx.x; i < 2 * a.D; i += 64 * kWaves) {
+        for (int i = threadIdx.x; i < 2 * a.D; i += 64 * WAVES) {
             const int j = i < a.D ? i : i - a.D + LPH * VEC;
-            dst[i] = sums[0][j] + sums[1][j] + sums[2][j] + sums[3][j];
+            float v = sums[0][j];
+#pragma unroll
+            for (int n = 1; n < WAVES; ++n) v += sums[n][j];
+            if constexpr (WAVES == kWaves)
+                dst[i] = v;
+            else
+                (i < a.D ? a.dwq : a.dwk)[i < a.D ? i : i - a.D] = v;
         }
     }
 }
@@ -159,12 +173,19 @@ struct Plan {
     int shares, blocks;
 };
 
+// Groups of a token's heads: loads of a wavefront.
+int groups_of(const lory_rope_shape &s)
+{
+    const int lph = s.dtype == LORY_F32 ? lanes_per_head<float>(s.head_dim) : lanes_per_head<__hip_bfloat16>(s.head_dim);
+    const int hpw = 64 / lph;
+    return (s.q_heads + hpw - 1) / hpw + (s.kv_heads + hpw - 1) / hpw;
+}
+
 // A token's heads over as many wavefronts as end first: rounds of the items over 4 kMaxBlocks wavefronts, each as long as
 // its groups and about one more for the angles.
 Plan plan(const lory_rope_shape &s)
 {
-    const int lph = s.dtype == LORY_F32 ? lanes_per_head<float>(s.head_dim) : lanes_per_head<__hip_bfloat16>(s.head_dim);
-    const int hpw = 64 / lph, groups = (s.q_heads + hpw - 1) / hpw + (s.kv_heads + hpw - 1) / hpw, waves = kWaves * kMaxBlocks;
+    const int groups = groups_of(s), waves = kWaves * kMaxBlocks;
     Plan p = {1, 0};
     if (s.tokens <= 0) return p;
     long best = 0;
@@ -180,27 +201,32 @@ Plan plan(const lory_rope_shape &s)
     return p;
 }
 
-template <typename T, int LPH> void launch2(const Args &a, int blocks, bool inter, bool norm, hipStream_t st)
+template <typename T, int LPH, bool INTER> void launch3(const Args &a, int blocks, bool norm, bool alone, hipStream_t st)
 {
-    const dim3 grid(blocks), block(64 * kWaves);
-    if (inter && norm)
-        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, true, true>), grid, block, 0, st, a);
-    else if (inter)
-        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, true, false>), grid, block, 0, st, a);
+    if (alone)
+        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, INTER, true, kAlone>), dim3(1), dim3(64 * kAlone), 0, st, a);
     else if (norm)
-        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, false, true>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, INTER, true, kWaves>), dim3(blocks), dim3(64 * kWaves), 0, st, a);
     else
-        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, false, false>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((qk_rope_bwd_kernel<T, LPH, INTER, false, kWaves>), dim3(blocks), dim3(64 * kWaves), 0, st, a);
 }
 
-template <typename T> void launch1(const Args &a, int blocks, bool inter, bool norm, hipStream_t st)
+template <typename T, int LPH> void launch2(const Args &a, int blocks, bool inter, bool norm, bool alone, hipStream_t st)
+{
+    if (inter)
+        launch3<T, LPH, true>(a, blocks, norm, alone, st);
+    else
+        launch3<T, LPH, false>(a, blocks, norm, alone, st);
+}
+
+template <typename T> void launch1(const Args &a, int blocks, bool inter, bool norm, bool alone, hipStream_t st)
 {
     switch (lanes_per_head<T>(a.D)) {
-    case 8: launch2<T, 8>(a, blocks, inter, norm, st); break;
-    case 16: launch2<T, 16>(a, blocks, inter, norm, st); break;
-    case 32: launch2<T, 32>(a, blocks, inter, norm, st); break;
+    case 8: launch2<T, 8>(a, blocks, inter, norm, alone, st); break;
+    case 16: launch2<T, 16>(a, blocks, inter, norm, alone, st); break;
+    case 32: launch2<T, 32>(a, blocks, inter, norm, alone, st); break;
     default:
-        if constexpr (sizeof(T) == 4) launch2<T, 64>(a, blocks, inter, norm, st);
+        if constexpr (sizeof(T) == 4) launch2<T, 64>(a, blocks, inter, norm, alone, st);
     }
 }
 
@@ -229,6 +255,8 @@ int qk_rope_bwd_launch(const lory_rope_shape &s, const lory_heads &q, const lory
     a.wq = wq;
     a.wk = wk;
     a.part = (float *)ws;
+    a.dwq = dwq;
+    a.dwk = dwk;
     a.tokens = s.tokens;
     a.shares = p.shares;
     a.Hq = s.q_heads;
@@ -239,13 +267,18 @@ int qk_rope_bwd_launch(const lory_rope_shape &s, const lory_heads &q, const lory
     const double values = (double)s.tokens * (s.q_heads + s.kv_heads) * s.head_dim;
     prof::Range r(st, prof::kQkRopeBwd, 17.0 * values, (wq ? 3.0 : 2.0) * esize * values + 4.0 * s.tokens);
     const bool inter = s.interleaved != 0, norm = wq != nullptr;
+    const bool alone = norm && s.tokens > 0 && s.tokens <= kAlone && 3.0 * esize * values <= kAloneBytes;
+    if (alone) {
+        const int groups = groups_of(s), shares = kAlone / s.tokens;
+        a.shares = shares < groups ? shares : groups;
+    }
     if (p.blocks > 0) {
         if (s.dtype == LORY_F32)
-            launch1<float>(a, p.blocks, inter, norm, st);
+            launch1<float>(a, p.blocks, inter, norm, alone, st);
         else
-            launch1<__hip_bfloat16>(a, p.blocks, inter, norm, st);
+            launch1<__hip_bfloat16>(a, p.blocks, inter, norm, alone, st);
     }
-    if (norm)
+    if (norm && !alone)
         hipLaunchKernelGGL(qk_rope_dw_kernel, dim3(2 * s.head_dim / kDwColumns), dim3(1024), 0, st, (const float *)ws, p.blocks,
                            s.head_dim, dwq, dwk);
     return launch_status();

@@ -208,6 +208,14 @@ def test_rope_gradient(n, Hq, Hkv, D, rot, inter, dtype):
     assert d2[0] is inplace and torch.equal(inplace, got[0])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,Hq,Hkv,D", [(1, 3, 1, 80), (5, 7, 3, 96), (16, 2, 1, 64), (17, 2, 1, 64), (16, 5, 1, 128), (2, 40, 2, 128),
+                                        (1, 80, 5, 256), (16, 1, 1, 8)])
+def test_rope_gradient_of_few_tokens(n, Hq, Hkv, D, dtype):
+    """Tokens and bytes on both sides of where one workgroup takes them all."""
+    test_rope_gradient(n, Hq, Hkv, D, D // 16 * 16, False, dtype)
+
+
 def test_rope_gradient_against_differences():
     """Central differences of the operator's own forward: the truncation is h^2 / 6 of third derivatives of order 1, the
     rounding that of the 64 values that change, of order 2 with their gradient: 64 * 2 * 24 * 2^-24 / (2 h); with
