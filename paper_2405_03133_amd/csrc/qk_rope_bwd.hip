@@ -88,7 +88,8 @@ template <typename T, int LPH, bool INTER, bool NORM, int WAVES> __global__ __la
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) y[e] = fmaf(dy[e], c[e], p[e] * s[e]);
                     if constexpr (NORM) {
-                        float x[VEC], xx = 0.f, gx = 0.f;
+                        // not 0 where no head is: an infinite r, without eps, would make NaN of its zeros
+                        float x[VEC], xx = h < H ? 0.f : 1.f, gx = 0.f;
                         widen<T>(rx[u], x);
 #pragma unroll
                         for (int e = 0; e < VEC; ++e) {
