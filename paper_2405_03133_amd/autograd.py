@@ -16,6 +16,13 @@ import torch
 from . import binding as lb
 
 
+def _gradient(g: torch.Tensor) -> torch.Tensor:
+    """A gradient as autograd hands it over, contiguous and 16-byte aligned as the library wants it: a contiguous view into a
+    larger one (that of a torch.cat) may start anywhere."""
+    g = g.contiguous()
+    return g if g.data_ptr() % 16 == 0 else g.clone()
+
+
 class _LoryLayer(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, R, Wg, Wu, Wd, T, save_merged):
@@ -41,7 +48,7 @@ class _LoryLayer(torch.autograd.Function):
         x, R, Wg, Wu, Wd, w, hbar, G, U = ctx.saved_tensors
         T = ctx.T
         d_ff = Wg.shape[2]
-        dX, dWg, dWu, dWd, dw = lb.lory_merged_ffn_bwd(x, w, Wg, Wu, Wd, dy.contiguous(), T, G_save=G, U_save=U,
+        dX, dWg, dWu, dWd, dw = lb.lory_merged_ffn_bwd(x, w, Wg, Wu, Wd, _gradient(dy), T, G_save=G, U_save=U,
                                                        grad_dtype=Wg.dtype, Wbar_save=ctx.Wbar)
         dR = lb.lory_route_bwd(R, w, hbar, dw, dX, T, d_ff=d_ff)   # adds the router path into dX
         return dX, dR.to(R.dtype), dWg, dWu, dWd, None, None
@@ -76,7 +83,7 @@ class _QkRope(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dq_out, dk_out):
         q, k, pos, freq, wq, wk = ctx.saved_tensors
-        dq, dk, dwq, dwk = lb.lory_qk_rope_bwd(q, k, dq_out.contiguous(), dk_out.contiguous(), pos, freq, wq, wk, ctx.eps,
+        dq, dk, dwq, dwk = lb.lory_qk_rope_bwd(q, k, _gradient(dq_out), _gradient(dk_out), pos, freq, wq, wk, ctx.eps,
                                                ctx.interleaved)
         if wq is not None:
             dwq, dwk = dwq.to(wq.dtype), dwk.to(wk.dtype)
