@@ -435,6 +435,10 @@ int lory_qk_rope_bwd(const lory_rope_shape *shape, const lory_heads *q, const lo
  * With a status other than 0 nothing is planned: table and free stay, lens_new =
  * lens, count_new = count, cu = 0, positions = 0, slots = -1.  The status
  * stays on the device: nothing waits for it.
+ * New tokens are packed: token i (of positions and slots, and of a program's
+ * queries) is that of the row b with cu[b] <= i < cu[b + 1], and rows that have
+ * ended or add nothing have none.  A call of lory_paged_attn on these tokens takes table[b]
+ * and positions[i] + 1 as the table and length of its row i.
  * All arrays are int32 except slots.  No output may overlap another array
  * (LORY_ERR_OVERLAP): a program keeps two sets of lens and count and swaps them.
  * Calling again with the same lens, add and count gives the same plan.

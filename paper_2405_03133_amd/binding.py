@@ -461,7 +461,8 @@ def lory_kv_plan(lens: torch.Tensor, add: torch.Tensor, table: torch.Tensor, fre
                  page: int, lens_new: torch.Tensor, cu: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor,
                  count_new: torch.Tensor, status: torch.Tensor) -> torch.Tensor:
     """Pages, positions and slots of a step's new tokens from the rows' lengths (add < 0: the row has ended), and the
-    pages that come back; int32 but slots (int64).  Returns status [1]: 0, or why nothing was planned (include/lory.h)."""
+    pages that come back; int32 but slots (int64).  Tokens are packed: token i is that of row b with cu[b] <= i < cu[b + 1],
+    and ended rows have none.  Returns status [1]: 0, or why nothing was planned (include/lory.h)."""
     _check(_native().kv_plan(lens, add, table, free, count, page, lens_new, cu, positions, slots, count_new, status),
            "lory_kv_plan")
     return status
@@ -487,7 +488,8 @@ def lory_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
                     workspace: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
     """out [rows, q_heads, head_dim] = attention of one token per row, q, over the first lens[b] tokens that table [rows,
     width] finds in the caches [pages, kv_heads, page, head_dim]; lse [rows, q_heads] fp32 receives the log of
-    the sum of exponentials.  scale is 1/sqrt(head_dim) unless given."""
+    the sum of exponentials.  scale is 1/sqrt(head_dim) unless given.  Row b of q goes with row b of table and lens: the
+    packed tokens of lory_kv_plan are other rows once one has ended or adds nothing."""
     status, out = _native().paged_attn(q, k_cache, v_cache, table, lens, scale, out, lse, workspace)
     _check(status, "lory_paged_attn")
     return out

@@ -1,12 +1,18 @@
 """The attention operators where a value, a layout or a step is out of the ordinary.  Plain implementations in 64 bits; bounds
 as in test_attn_gpu.py."""
+import os
+import re
+
+import numpy as np
 import pytest
 import torch
 
 import test_attn_gpu as base
 from paper_2405_03133_amd import autograd
-from test_attn_gpu import T, freqs, gen, rnd
+from paper_2405_03133_amd import binding as lb
+from test_attn_gpu import T, check_attention, freqs, gen, rnd
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 pytestmark = pytest.mark.gpu
 
 
@@ -47,3 +53,45 @@ def test_gradients_at_any_address(dtype):
     layer = lambda x, R, Wg, Wu, Wd: [autograd.lory_layer(x, R, Wg, Wu, Wd, seg)]
     for a, b in zip(grads(layer, leaves, 0), grads(layer, leaves, 1)):
         assert torch.equal(a, b)
+
+
+def test_generation_snippet_of_the_readme_with_a_row_that_has_ended():
+    """A step's tokens are packed, and a row that has ended has none: the rows behind it still attend with their own queries."""
+    text = open(os.path.join(ROOT, "README.md")).read()
+    code = re.search(r"^Generation:.*?```python\n(.*?)```", text, re.S | re.M).group(1)
+    B, W, page, F, Hq, Hkv, D = 5, 8, 16, 60, 4, 2, 64
+    g = gen(40)
+    i32 = lambda a: torch.tensor(np.asarray(a).tolist(), dtype=torch.int32, device="cuda")
+    held, add = [40, 17, 64, 5, 99], [1, -1, 1, -1, 1]
+    blocks = [-(-n // page) for n in held]
+    pages = np.random.RandomState(1).permutation(F)
+    table, at = np.full((B, W), -1), 0
+    for b, m in enumerate(blocks):
+        table[b, :m] = pages[at:at + m]
+        at += m
+    free = np.full(F, -1)
+    free[:F - at] = pages[at:]
+    k_cache, v_cache = rnd(g, F, Hkv, page, D), rnd(g, F, Hkv, page, D)
+    old = table.copy()
+    qkv = rnd(g, B, (Hq + 2 * Hkv) * D)
+    q, k, v = (x.unflatten(1, (-1, D)) for x in qkv.split([Hq * D, Hkv * D, Hkv * D], 1))
+    s = dict(torch=torch, lb=lb, lens=i32(held), add=i32(add), table=i32(table), free=i32(free), count=i32([F - at]), page=page,
+             lens_new=i32([0] * B), cu=i32([0] * (B + 1)), positions=i32([0] * B), slots=torch.zeros(B, dtype=torch.int64, device="cuda"),
+             count_new=i32([0]), status=i32([0]), q=q, k=k, v=v, freq=freqs(D), wq=1 + rnd(g, D) / 4, wk=1 + rnd(g, D) / 4,
+             k_cache=k_cache, v_cache=v_cache)
+    exec(code, s)
+    assert s["status"].item() == 0
+    live = [0, 2, 4]
+    # the packed token i is that of the i-th live row: its query over that row's cache, the new key and value among them
+    pos = i32([held[b] for b in live])
+    yq, yk = lb.lory_qk_rope(q[:3], k[:3], pos, s["freq"], wq=s["wq"], wk=s["wk"])
+    assert torch.equal(s["q"][:3], yq)
+    for i, b in enumerate(live):
+        row, n = s["table"][b], held[b] + 1
+        assert row[:blocks[b]].tolist() == old[b, :blocks[b]].tolist()
+        slot = int(row[held[b] // page]) * page + held[b] % page
+        assert torch.equal(k_cache[slot // page, :, slot % page], yk[i]) and torch.equal(v_cache[slot // page, :, slot % page], v[i])
+        lse = torch.empty(1, Hq, device="cuda")
+        lb.lory_paged_attn(yq[i:i + 1], k_cache, v_cache, row[None], i32([n]), lse=lse)
+        check_attention(f"row {b}", s["out"][i:i + 1], lse, yq[i:i + 1], k_cache, v_cache, row[None], i32([n]))
+    assert (s["out"][3:] == 0).all()   # places without a token
