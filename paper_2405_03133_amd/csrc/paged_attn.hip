@@ -29,6 +29,8 @@
 // a ragged batch takes 55 us instead of 31, with agent-scope loads and stores 34.
 #include <hip/hip_bf16.h>
 
+#include <type_traits>
+
 #include "gemm_bf16.h"
 #include "lory_internal.h"
 #include "paged_index.h"
@@ -197,7 +199,8 @@ template <int DP, bool PAD> struct Wave<__hip_bfloat16, DP, PAD> {
                 for (int e = 0; e < VW / 2; ++e) x.v[j][m][e] = on ? x.v[j][m][e] : 0;
         }
     }
-    __device__ void add(const Keys &x, const float (&p)[8])
+    // SPLIT: an infinite value counts with hi alone (a lo of 0 or of the other sign would make NaN of it)
+    template <bool SPLIT> __device__ void add(const Keys &x, const float (&p)[8])
     {
         u32x4 hi, lo;
 #pragma unroll
@@ -215,8 +218,25 @@ template <int DP, bool PAD> struct Wave<__hip_bfloat16, DP, PAD> {
                                              (t & 1) ? 0x07060302u : 0x05040100u);
             const bf16x8 af = __builtin_bit_cast(bf16x8, y);
             o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af, bh, o[t], 0, 0, 0);
-            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(af, bl, o[t], 0, 0, 0);
+            if constexpr (SPLIT) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    if ((y[n] & 0x7f80u) == 0x7f80u) y[n] &= 0xffff0000u;
+                    if ((y[n] & 0x7f800000u) == 0x7f800000u) y[n] &= 0xffffu;
+                }
+            }
+            o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, y), bl, o[t], 0, 0, 0);
         }
+    }
+    // the lane's sums have an infinity or NaN among them (or are large enough to make one)
+    __device__ bool odd() const
+    {
+        f32x4 v = o[0];
+#pragma unroll
+        for (int t = 1; t < NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += o[t][e];
+        return !(fabsf((v[0] + v[1]) + (v[2] + v[3])) < INFINITY);
     }
 };
 
@@ -285,7 +305,7 @@ template <int DP, bool PAD> struct Wave<float, DP, PAD> {
                 for (int e = 0; e < 4; ++e) x.v[j][m][e] = on ? x.v[j][m][e] : 0.f;
         }
     }
-    __device__ void add(const Keys &x, const float (&p)[4])
+    template <bool> __device__ void add(const Keys &x, const float (&p)[4])
     {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
@@ -336,60 +356,68 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
     auto row_of = [&](int at, int page) {
         return paged::cache_row(a.div, at + (lane & (KEYS - 1)), page, a.pages, a.Hkv, kvh);
     };
-    typename W::Keys x;
-    int at = t0 * kTile<T> + wave * KEYS;
-    int page = page_of(at), next = page_of(at + STEP);
+    const int at0 = t0 * kTile<T> + wave * KEYS, page0 = page_of(at0), page1 = page_of(at0 + STEP);
     w.load_q(a.q + b * a.q_row + (first + i) * a.q_head, a.D, c, i < nq);
+    float m, l;
+    auto walk = [&](auto split, int page, int next) {
+        typename W::Keys x;
+        int at = at0;
 #pragma unroll
-    for (int t = 0; t < W::NT; ++t) w.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
+        for (int t = 0; t < W::NT; ++t) w.o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m = -INFINITY;
+        l = 0.f;
 
-    int row = row_of(at, page);
-    if (at < last) {
-        W::load_k(x, a.k, max(row, 0), a.D, i, c);
-        W::template load_v<STREAM>(x, a.v, max(row, 0), a.D, i, c);
-    }
-    for (; at < last; at += STEP) {
+        int row = row_of(at, page);
+        if (at < last) {
+            W::load_k(x, a.k, max(row, 0), a.D, i, c);
+            W::template load_v<STREAM>(x, a.v, max(row, 0), a.D, i, c);
+        }
+        for (; at < last; at += STEP) {
 #pragma clang fp contract(off)
-        const uint32_t valid = (uint32_t)__ballot(row >= 0), every = (uint32_t)((1ull << KEYS) - 1);
-        row = row_of(at + STEP, next);
-        next = page_of(at + 2 * STEP);
-        const bool more = at + STEP < last;
+            const uint32_t valid = (uint32_t)__ballot(row >= 0), every = (uint32_t)((1ull << KEYS) - 1);
+            row = row_of(at + STEP, next);
+            next = page_of(at + 2 * STEP);
+            const bool more = at + STEP < last;
 
-        float s[NS];
-        w.scores(x, s);
-        if (more) W::load_k(x, a.k, max(row, 0), a.D, i, c);
+            float s[NS];
+            w.scores(x, s);
+            if (more) W::load_k(x, a.k, max(row, 0), a.D, i, c);
 
-        // rounded before the maximum is taken off: equal scores of any size stay equal (a fused product would not)
+            // rounded before the maximum is taken off: equal scores of any size stay equal (a fused product would not)
 #pragma unroll
-        for (int n = 0; n < NS; ++n) s[n] *= a.scale2;
-        if (valid != every) {
-            W::clear_v(x, valid, c);
+            for (int n = 0; n < NS; ++n) s[n] *= a.scale2;
+            if (valid != every) {
+                W::clear_v(x, valid, c);
 #pragma unroll
-            for (int n = 0; n < NS; ++n)
-                if (!((valid >> ((n >> 2) * 16 + 4 * c + (n & 3))) & 1)) s[n] = -INFINITY;
+                for (int n = 0; n < NS; ++n)
+                    if (!((valid >> ((n >> 2) * 16 + 4 * c + (n & 3))) & 1)) s[n] = -INFINITY;
+            }
+            float top = s[0];
+#pragma unroll
+            for (int n = 1; n < NS; ++n) top = fmaxf(top, s[n]);
+            const float m1 = fmaxf(m, xor_max(top));
+            const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing but -inf so far: every weight is 0
+            if (__any(m1 != m)) {
+                const float f = __builtin_amdgcn_exp2f(m - ref);
+                l *= f;
+#pragma unroll
+                for (int t = 0; t < W::NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w.o[t][e] *= f;
+            }
+            m = m1;
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                s[n] = __builtin_amdgcn_exp2f(s[n] - ref);
+                l += s[n];
+            }
+            w.template add<decltype(split)::value>(x, s);
+            if (more) W::template load_v<STREAM>(x, a.v, max(row, 0), a.D, i, c);
         }
-        float top = s[0];
-#pragma unroll
-        for (int n = 1; n < NS; ++n) top = fmaxf(top, s[n]);
-        const float m1 = fmaxf(m, xor_max(top));
-        const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing but -inf so far: every weight is 0
-        if (__any(m1 != m)) {
-            const float f = __builtin_amdgcn_exp2f(m - ref);
-            l *= f;
-#pragma unroll
-            for (int t = 0; t < W::NT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) w.o[t][e] *= f;
-        }
-        m = m1;
-#pragma unroll
-        for (int n = 0; n < NS; ++n) {
-            s[n] = __builtin_amdgcn_exp2f(s[n] - ref);
-            l += s[n];
-        }
-        w.add(x, s);
-        if (more) W::template load_v<STREAM>(x, a.v, max(row, 0), a.D, i, c);
+    };
+    walk(std::false_type(), page0, page1);
+    if constexpr (sizeof(T) == 2) {   // infinite values among these keys: once more, with what they take in every step
+        if (__builtin_expect(__any(i < nq && w.odd()), 0)) walk(std::true_type(), page_of(at0), page_of(at0 + STEP));
     }
     l = xor_sum(l);
 

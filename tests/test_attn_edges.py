@@ -10,7 +10,7 @@ import torch
 import test_attn_gpu as base
 from paper_2405_03133_amd import autograd
 from paper_2405_03133_amd import binding as lb
-from test_attn_gpu import T, check_attention, freqs, gen, rnd
+from test_attn_gpu import T, attend, check_attention, freqs, gen, paged_case, rnd
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 pytestmark = pytest.mark.gpu
@@ -95,3 +95,28 @@ def test_generation_snippet_of_the_readme_with_a_row_that_has_ended():
         lb.lory_paged_attn(yq[i:i + 1], k_cache, v_cache, row[None], i32([n]), lse=lse)
         check_attention(f"row {b}", s["out"][i:i + 1], lse, yq[i:i + 1], k_cache, v_cache, row[None], i32([n]))
     assert (s["out"][3:] == 0).all()   # places without a token
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,Hq,Hkv,D,page", [([1, 37, 200], 2, 1, 64, 16), ([1, 130, 9], 17, 1, 40, 8), ([5000, 1, 64], 8, 2, 128, 16),
+                                                ([1, 300], 4, 2, 256, 16), ([333, 4000], 20, 4, 80, 24)])
+def test_attention_of_infinite_values(lens, Hq, Hkv, D, page, dtype):
+    """A value of a token that counts may be infinite: so is its dim of every query of the head, NaN where both signs meet;
+    all other dims are what they are without it."""
+    q, k, v, table, dlens = paged_case(sum(lens), lens, Hq, Hkv, D, page, dtype, sigma=0.5)
+    plain = attend((q, k, v, table, dlens))
+    inf = float("inf")
+    v = v.clone()
+    for b, n in enumerate(lens):
+        for t, d, x in ((0, 0, inf), (n - 1, D - 1, -inf), (n // 2, D // 2, inf), (n // 3, 5, inf), (n - 1, 5, -inf), (n // 4, 6, float("nan"))):
+            if n > 1 or d != 5:
+                v[int(table[b, t // page]), Hkv - 1, t % page, d] = x
+    out, lse = attend((q, k, v, table, dlens))
+    check_attention("infinite values", out, lse, q, k, v, table, dlens)
+    last = out[:, -(Hq // Hkv):]
+    for b, n in enumerate(lens):
+        assert (last[b, :, 0] == inf).all() and (last[b, :, D - 1] == -inf).all() and (last[b, :, D // 2] == inf).all()
+        assert torch.isnan(last[b, :, 6]).all() and (n == 1 or torch.isnan(last[b, :, 5]).all())
+    odd = torch.zeros(D, dtype=torch.bool, device="cuda")
+    odd[[0, 5, 6, D // 2, D - 1]] = True
+    assert torch.equal(lse, plain[1]) and torch.equal(out[..., ~odd], plain[0][..., ~odd])
