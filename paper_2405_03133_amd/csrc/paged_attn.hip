@@ -68,7 +68,7 @@ struct Args {
     int group, tiles;         // query heads of a key-value head, and blocks of 16 of them
     int groups;               // ranges that share the units
     paged::Divider div;       // by page
-    float scale2;             // scale * log2(e)
+    float scale;
 };
 
 // Values are read past the caches where the key-value cache is too large to be found in the memory-side cache (256 MB, of which
@@ -98,6 +98,9 @@ template <typename T> __device__ __forceinline__ int units_of(int len)
 {
     return len <= kTile<T> ? 1 : (len + kTile<T> - 1) / kTile<T>;   // an empty row has one, which writes its zeros
 }
+
+// e^x for x <= 0
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 __device__ __forceinline__ float xor_max(float v)
 {
@@ -330,7 +333,7 @@ template <typename T> __device__ __forceinline__ void write_out(const Args &a, i
         *reinterpret_cast<uint32_t *>(p) = gemm::cvt_pk_bf16(O0 / n, O1 / n);
     else
         *reinterpret_cast<float2 *>(p) = make_float2(O0 / n, O1 / n);
-    if (d == 0 && a.lse) a.lse[(long)b * a.Hq + head] = (ref + log2f(L)) * kLn2;
+    if (d == 0 && a.lse) a.lse[(long)b * a.Hq + head] = fmaf(log2f(L), kLn2, ref);
 }
 
 // Tiles t0 .. t1 of head h (a block of up to 16 query heads of a key-value head) of row b, whose length is len: the
@@ -383,9 +386,10 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             w.scores(x, s);
             if (more) W::load_k(x, a.k, max(row, 0), a.D, i, c);
 
-            // rounded before the maximum is taken off: equal scores of any size stay equal (a fused product would not)
+            // rounded before the maximum is taken off: equal scores of any size stay equal (a fused product would not); to
+            // base 2 only then, so that a score counts as long as fp32 holds it
 #pragma unroll
-            for (int n = 0; n < NS; ++n) s[n] *= a.scale2;
+            for (int n = 0; n < NS; ++n) s[n] *= a.scale;
             if (valid != every) {
                 W::clear_v(x, valid, c);
 #pragma unroll
@@ -398,7 +402,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             const float m1 = fmaxf(m, xor_max(top));
             const float ref = m1 == -INFINITY ? 0.f : m1;   // nothing but -inf so far: every weight is 0
             if (__any(m1 != m)) {
-                const float f = __builtin_amdgcn_exp2f(m - ref);
+                const float f = exp_of(m - ref);
                 l *= f;
 #pragma unroll
                 for (int t = 0; t < W::NT; ++t)
@@ -408,7 +412,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             m = m1;
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
-                s[n] = __builtin_amdgcn_exp2f(s[n] - ref);
+                s[n] = exp_of(s[n] - ref);
                 l += s[n];
             }
             w.template add<decltype(split)::value>(x, s);
@@ -442,7 +446,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
         float L = 0.f, O0 = 0.f, O1 = 0.f;
 #pragma unroll
         for (int n = 0; n < NW; ++n) {
-            const float f = __builtin_amdgcn_exp2f(sh.m[n][j] - ref);
+            const float f = exp_of(sh.m[n][j] - ref);
             L = fmaf(f, sh.l[n][j], L);
             O0 = fmaf(f, sh.o[n][j][d], O0);
             O1 = fmaf(f, sh.o[n][j][d + 1], O1);
@@ -570,7 +574,7 @@ template <typename T, bool BY_ROW> __global__ __launch_bounds__(kJoinThreads) vo
             f32x4 O = {0.f, 0.f, 0.f, 0.f};
             auto take = [&](float m, float l, f32x4 o) {
                 const float M1 = fmaxf(M, m), ref = M1 == -INFINITY ? 0.f : M1;
-                const float f = __builtin_amdgcn_exp2f(M - ref), g = __builtin_amdgcn_exp2f(m - ref);
+                const float f = exp_of(M - ref), g = exp_of(m - ref);
                 L = L * f + l * g;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) O[e] = O[e] * f + o[e] * g;
@@ -739,7 +743,7 @@ int paged_attn_launch(const lory_paged_shape &s, const lory_heads &q, const void
     a.group = s.q_heads / s.kv_heads;
     a.tiles = (a.group + 15) / 16;
     a.div = paged::divider(s.page);
-    a.scale2 = s.scale * kLog2e;
+    a.scale = s.scale;
     prof::Range r(st, prof::kPagedAttn, 0.0, 0.0);   // the lengths are on the device
     if (s.dtype == LORY_F32)
         launch1<float>(a, p, st);

@@ -10,7 +10,7 @@ import torch
 import test_attn_gpu as base
 from paper_2405_03133_amd import autograd
 from paper_2405_03133_amd import binding as lb
-from test_attn_gpu import T, attend, check_attention, freqs, gen, paged_case, rnd
+from test_attn_gpu import E32, T, attend, check_attention, freqs, gen, paged_case, rnd, within
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 pytestmark = pytest.mark.gpu
@@ -120,3 +120,35 @@ def test_attention_of_infinite_values(lens, Hq, Hkv, D, page, dtype):
     odd = torch.zeros(D, dtype=torch.bool, device="cuda")
     odd[[0, 5, 6, D // 2, D - 1]] = True
     assert torch.equal(lse, plain[1]) and torch.equal(out[..., ~odd], plain[0][..., ~odd])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("scale", [0.5, 0.7, 1.0])
+@pytest.mark.parametrize("lens", [[200, 1, 65], [9000, 200, 3]])
+def test_attention_scores_at_the_ends_of_their_range(lens, scale, sign, dtype):
+    """Head 0's scores are all scale times the type's lowest (or largest) value; head 1's are that and, every third, 0.  Any
+    score that fp32 holds counts as it is: equal ones weigh alike, and beside a 0 the lowest ones nothing."""
+    t, D, page = T[dtype], 64, 16
+    q, k, v, table, dlens = paged_case(7 + len(lens), lens, 2, 2, D, page, dtype, sigma=1.0)
+    end = sign * torch.finfo(t).max
+    q.zero_()
+    q[..., 0] = 1
+    for b, n in enumerate(lens):
+        i = torch.arange(n, device="cuda")
+        p = table[b].long()[i // page]
+        k[p, :, i % page] = 0
+        k[p, 0, i % page, 0] = end
+        k[p, 1, i % page, 0] = torch.where(i % 3 == 0, 0.0, end).to(t)
+    out, lse = attend((q, k, v, table, dlens), scale=scale)
+    for b, n in enumerate(lens):
+        i = torch.arange(n, device="cuda")
+        V = v[table[b].long()[i // page], :, i % page].double()
+        for h in range(2):
+            keep = torch.ones_like(i, dtype=torch.bool) if h == 0 else i % 3 == 0 if sign < 0 else (i % 3 != 0) | (n == 1)
+            ref = V[keep, h].mean(0)
+            # as the plain means of test_attention_extreme_scores; sums of equal weights in chains of at most n / 16 + 64
+            within(f"{n} scores, head {h}", out[b, h], ref, (2.0 ** -16 + (8 + 2 * (n / 16 + 64)) * E32) * V[keep, h].abs().mean(0), t)
+            top = 0.0 if h == 1 and (sign < 0 or n == 1) else scale * end
+            want = top + float(np.log(keep.sum().item()))
+            assert abs(lse[b, h].item() - want) <= (4 + n / 16 + 64 + 8 * abs(want)) * E32, (n, h, lse[b, h].item(), want)
