@@ -377,7 +377,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
         }
         for (; at < last; at += STEP) {
 #pragma clang fp contract(off)
-            const uint32_t valid = (uint32_t)__ballot(row >= 0), every = (uint32_t)((1ull << KEYS) - 1);
+            const uint32_t valid = paged::valid_keys(__ballot(row >= 0), KEYS);
             row = row_of(at + STEP, next);
             next = page_of(at + 2 * STEP);
             const bool more = at + STEP < last;
@@ -390,7 +390,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             // base 2 only then, so that a score counts as long as fp32 holds it
 #pragma unroll
             for (int n = 0; n < NS; ++n) s[n] *= a.scale;
-            if (valid != every) {
+            if (valid != paged::all_keys(KEYS)) {
                 W::clear_v(x, valid, c);
 #pragma unroll
                 for (int n = 0; n < NS; ++n)

@@ -40,6 +40,11 @@ LORY_HD int cache_row(const Divider &d, uint32_t t, int at, int pages, int heads
     return (uint32_t)at < (uint32_t)pages ? (at * heads + head) * d.page + (int)(t - quotient(d, t) * d.page) : -1;
 }
 
+// Keys of a wavefront's step that have a page, as bits: its lanes' ballot, in which lanes behind the step's keys (16 of 64 in
+// fp32, 32 in bf16) repeat them.
+LORY_HD uint32_t all_keys(int keys) { return (uint32_t)(((uint64_t)1 << keys) - 1); }
+LORY_HD uint32_t valid_keys(uint64_t ballot, int keys) { return (uint32_t)ballot & all_keys(keys); }
+
 // a / b for 0 <= a, 0 < b; the 64-bit division takes some 150 instructions, the 32-bit one 30.
 LORY_HD long quotient64(long a, long b)
 {
