@@ -4,12 +4,13 @@
 //   dx = r g w - x r^3 / D * sum(g w x),   dw += g x r,
 // so both sums of a head (x^2 and g w x) come from the same registers.  Wavefronts walk over tokens and keep dw of their
 // chunk in registers; every workgroup adds its wavefronts in LDS and leaves one row of partial sums, and a second
-// launch adds the rows in order: the same bits on every run.  A few tokens take one workgroup, and that launch only (kAlone).
+// launch adds the rows in order: the same bits on every run.  A few tokens take one workgroup, and that launch only (qk_rope_plan.h).
 // 128 registers, four wavefronts per SIMD and 1024 workgroups, all resident at once: with 141 registers a quarter of them
 // waited for a second round (99 us against 79 for 16384 tokens of 32 heads of 128, bf16).  Workgroups of eight or 16 wavefronts leave
 // fewer rows to add but measured the same or slower (79.6, 86).
 // Measured: those 16384 tokens 73.4 us, 5.5 TB/s, and 4.6 us for the rows; 2999 fp32 tokens of 24 + 8 heads of 64 16.6 + 3.9 us.
 #include "qk_rope.h"
+#include "qk_rope_plan.h"
 
 namespace lory {
 
@@ -18,12 +19,6 @@ namespace {
 using namespace rope;
 
 constexpr int kMaxBlocks = 1024;   // rows of partial sums
-// A few tokens with norms take one workgroup of 16 wavefronts, which writes dw itself, and no second launch: at most 16 tokens, a
-// wavefront each, and kAloneBytes of heads and gradients read and written, as one CU moves about 60 bytes per ns.  Called eagerly
-// and from a graph, one launch against two: bf16 15 KB 7.1 and 4.7 us against 9.7 and 6.5, 60 KB 7.1 and 6.5 against 9.8 and 6.5,
-// 120 KB 7.8 and 7.7 against 9.8 and 6.6, 240 KB 9.8 and 9.8 against 9.8 and 6.6.
-constexpr int kAlone = 16;
-constexpr long kAloneBytes = 128 << 10;
 
 struct Args {
     Heads q, k, dyq, dyk, dq, dk;
@@ -268,7 +263,7 @@ int qk_rope_bwd_launch(const lory_rope_shape &s, const lory_heads &q, const lory
     const double values = (double)s.tokens * (s.q_heads + s.kv_heads) * s.head_dim;
     prof::Range r(st, prof::kQkRopeBwd, 17.0 * values, (wq ? 3.0 : 2.0) * esize * values + 4.0 * s.tokens);
     const bool inter = s.interleaved != 0, norm = wq != nullptr;
-    const bool alone = norm && s.tokens > 0 && s.tokens <= kAlone && 3.0 * esize * values <= kAloneBytes;
+    const bool alone = norm && rope::alone(s.tokens, (long)s.tokens * (s.q_heads + s.kv_heads) * s.head_dim);
     if (alone) {
         const int groups = groups_of(s), shares = kAlone / s.tokens;
         a.shares = shares < groups ? shares : groups;

@@ -40,3 +40,26 @@ int main()
 
 def test_a_step_with_all_its_keys_is_known_as_one(tmp_path):
     run_host(tmp_path, STEP)
+
+
+ALONE = r"""
+#include <stdio.h>
+#include "qk_rope_plan.h"
+using lory::rope::alone;
+int main()
+{
+    long bad = 0;
+    // tokens and values: one launch is up to a microsecond and more slower from a graph; it is faster, or slower by half of one at most
+    const long two[][2] = {{10, 10240}, {8, 10240}, {6, 15360}, {12, 15360}, {7, 17920}, {8, 20480}, {16, 20480}, {17, 136}};
+    const long one[][2] = {{1, 512}, {5, 2560}, {1, 2560}, {12, 6144}, {4, 5120}, {2, 5120}, {1, 5120}, {3, 7680}, {16, 8192}};
+    for (auto &c : two) bad += alone(c[0], c[1]);
+    for (auto &c : one) bad += !alone(c[0], c[1]);
+    bad += alone(0, 0) || alone(1l << 25, (1l << 25) * 131070 * 256);
+    printf("bad %ld\n", bad);
+    return bad != 0;
+}
+"""
+
+
+def test_one_workgroup_takes_a_gradient_only_where_replays_stand_it(tmp_path):
+    run_host(tmp_path, ALONE)
