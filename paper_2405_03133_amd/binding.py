@@ -416,7 +416,8 @@ def lory_qk_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, freq: torc
                  interleaved: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
     """Head norms with weights wq, wk [head_dim] (none without them) and position rotation of q [tokens, q_heads,
     head_dim] and k [tokens, kv_heads, head_dim]; pos [tokens] int32, freq [rot_dim/2] fp64 radians per
-    position.  Returns (q_out, k_out); an output may be its own input."""
+    position.  Returns (q_out, k_out); an output may be its own input.  As every call here it builds no graph, whatever its
+    inputs require (autograd.qk_rope does); outputs that are given count as changed in place."""
     status, q_out, k_out = _native().qk_rope(q, k, pos, freq, wq, wk, eps, interleaved, q_out, k_out)
     _check(status, "lory_qk_rope")
     return q_out, k_out
@@ -427,7 +428,7 @@ def lory_qk_rope_cache(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: t
                        q_out: Optional[torch.Tensor] = None, wq: Optional[torch.Tensor] = None,
                        wk: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False) -> torch.Tensor:
     """lory_qk_rope whose keys go, with the values v beside them, to slots [tokens] int64 of the caches [pages, kv_heads,
-    page, head_dim] (slot = page number * page + row; outside of them: not stored).  Returns q_out."""
+    page, head_dim] (slot = page number * page + row; outside of them: not stored).  Returns q_out.  Builds no graph."""
     status, q_out = _native().qk_rope_cache(q, k, pos, freq, wq, wk, eps, interleaved, v, k_cache, v_cache, slots, q_out)
     _check(status, "lory_qk_rope_cache")
     return q_out
@@ -489,7 +490,7 @@ def lory_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     """out [rows, q_heads, head_dim] = attention of one token per row, q, over the first lens[b] tokens that table [rows,
     width] finds in the caches [pages, kv_heads, page, head_dim]; lse [rows, q_heads] fp32 receives the log of
     the sum of exponentials.  scale is 1/sqrt(head_dim) unless given.  Row b of q goes with row b of table and lens: the
-    packed tokens of lory_kv_plan are other rows once one has ended or adds nothing."""
+    packed tokens of lory_kv_plan are other rows once one has ended or adds nothing.  Builds no graph."""
     status, out = _native().paged_attn(q, k_cache, v_cache, table, lens, scale, out, lse, workspace)
     _check(status, "lory_paged_attn")
     return out

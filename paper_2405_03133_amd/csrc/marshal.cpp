@@ -3,7 +3,8 @@
 // Calls of these operators take 4 us on the GPU at the least and up to fifteen tensors each; read through Python attributes and
 // ctypes their arguments cost 5 to 7 us of the host's time, here below one (the launch itself is 3.5).  Nothing is computed
 // and nothing kept: every function checks types, shapes, strides and devices, allocates outputs that were not
-// given, and passes addresses and the current stream to the C entry of the same name.  The documented functions
+// given, passes addresses and the current stream to the C entry of the same name, and counts the caller's outputs as
+// changed in place.  The documented functions
 // are those of binding.py, which also turns the status into an error.
 #include <Python.h>
 
@@ -31,6 +32,7 @@ struct Call {
     int device = -1;                   // of the first tensor
     const char *elsewhere = nullptr;   // an argument that is on no GPU, or on another one
     at::ScalarType type = at::kFloat;  // of the heads
+    int written[9], outputs = 0;       // arguments that the call writes into
 
     const at::Tensor &tensor(int i, const char *name)
     {
@@ -50,6 +52,21 @@ struct Call {
         const c10::hip::HIPStream s = c10::hip::getCurrentHIPStream();
         if (s.device_index() != device) raise(PyExc_ValueError, "the tensors must live on the current GPU");
         return (void *)s.stream();
+    }
+    // The caller's tensors at these places are outputs (None: a new one).
+    void writes(std::initializer_list<int> at)
+    {
+        for (const int i : at)
+            if (!none(i)) written[outputs++] = i;
+    }
+    // Status of the C entry.  Outputs have changed by now: autograd is to know if a graph had kept one of them.
+    int done(int status)
+    {
+        for (int i = 0; status == LORY_OK && i < outputs; ++i) {
+            const at::Tensor &t = THPVariable_Unpack(args[written[i]]);
+            if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+        }
+        return status;
     }
     void of_type(const at::Tensor &t, at::ScalarType want, const char *name)
     {
@@ -235,7 +252,8 @@ PyObject *qk_rope(Call &c)
     const at::Tensor tq = c.output(8, c.tensor(0, "q"), "q_out"), tk = c.output(9, c.tensor(1, "k"), "k_out");
     const lory_heads q = c.heads(tq, r.n, r.Hq, r.D, "q_out"), k = c.heads(tk, r.n, r.Hkv, r.D, "k_out");
     void *stream = c.stream();
-    return result(lory_qk_rope(&r.shape, &r.q, &r.k, r.pos, r.freq, r.wq, r.wk, &q, &k, stream), {tq, tk});
+    c.writes({8, 9});
+    return result(c.done(lory_qk_rope(&r.shape, &r.q, &r.k, r.pos, r.freq, r.wq, r.wk, &q, &k, stream)), {tq, tk});
 }
 
 // q, k, pos, freq, wq, wk, eps, interleaved, v, k_cache, v_cache, slots, q_out
@@ -249,8 +267,9 @@ PyObject *qk_rope_cache(Call &c)
     const at::Tensor tq = c.output(12, c.tensor(0, "q"), "q_out");
     const lory_heads q = c.heads(tq, r.n, r.Hq, r.D, "q_out");
     void *stream = c.stream();
-    return result(lory_qk_rope_cache(&r.shape, &r.q, &r.k, &v, r.pos, r.freq, r.wq, r.wk, &q, kc, vc, pages, page, slots, stream),
-                  {tq});
+    c.writes({9, 10, 12});
+    return result(c.done(lory_qk_rope_cache(&r.shape, &r.q, &r.k, &v, r.pos, r.freq, r.wq, r.wk, &q, kc, vc, pages, page, slots,
+                                            stream)), {tq});
 }
 
 // q, k, pos, freq, wq, wk, eps, interleaved, dq_out, dk_out, dq, dk, dwq, dwk, workspace
@@ -281,8 +300,9 @@ PyObject *qk_rope_bwd(Call &c)
         raise(PyExc_ValueError, "dwq and dwk need wq and wk");
     }
     void *stream = c.stream();
-    return result(lory_qk_rope_bwd(&r.shape, &r.q, &r.k, &dyq, &dyk, r.pos, r.freq, r.wq, r.wk, &dq, &dk, pw[0], pw[1], ws, bytes,
-                                   stream), {tq, tk, dw[0], dw[1]});
+    c.writes({10, 11, 12, 13});
+    return result(c.done(lory_qk_rope_bwd(&r.shape, &r.q, &r.k, &dyq, &dyk, r.pos, r.freq, r.wq, r.wk, &dq, &dk, pw[0], pw[1], ws,
+                                          bytes, stream)), {tq, tk, dw[0], dw[1]});
 }
 
 // lens, add, table, free, count, page, lens_new, cu, positions, slots, count_new, status
@@ -297,7 +317,8 @@ PyObject *kv_plan(Call &c)
                       nullptr, c.ints(10, 1, "count_new"), c.ints(11, 1, "status")};
     int64_t *slots = c.array<int64_t>(9, at::kLong, room, "slots");
     void *stream = c.stream();
-    return PyLong_FromLong(lory_kv_plan(&s, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], slots, p[9], p[10], stream));
+    c.writes({2, 3, 6, 7, 8, 9, 10, 11});
+    return PyLong_FromLong(c.done(lory_kv_plan(&s, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], slots, p[9], p[10], stream)));
 }
 
 // q, k_cache, v_cache, table, lens, scale, out, lse, workspace
@@ -336,7 +357,8 @@ PyObject *paged_attn(Call &c)
         ws = own.data_ptr();
     }
     void *stream = c.stream();
-    return result(lory_paged_attn(&s, &q, k, v, table, lens, &out, lse, ws, bytes, stream), {to});
+    c.writes({6, 7});
+    return result(c.done(lory_paged_attn(&s, &q, k, v, table, lens, &out, lse, ws, bytes, stream)), {to});
 }
 
 PyMethodDef methods[] = {

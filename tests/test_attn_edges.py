@@ -152,3 +152,36 @@ def test_attention_scores_at_the_ends_of_their_range(lens, scale, sign, dtype):
             top = 0.0 if h == 1 and (sign < 0 or n == 1) else scale * end
             want = top + float(np.log(keep.sum().item()))
             assert abs(lse[b, h].item() - want) <= (4 + n / 16 + 64 + 8 * abs(want)) * E32, (n, h, lse[b, h].item(), want)
+
+
+def test_writes_are_seen_by_autograd():
+    """Tensors that a call writes into count as changed: a graph that kept one of them raises instead of using the new values."""
+    g = gen(50)
+    n, H, D, page = 4, 2, 64, 16
+    x, pos, freq, w = rnd(g, n, H, D), torch.arange(n, device="cuda", dtype=torch.int32), freqs(64), torch.ones(D, device="cuda")
+    kc, vc = torch.zeros(2, H, page, D, device="cuda"), torch.zeros(2, H, page, D, device="cuda")
+    table, slots = torch.zeros(n, 1, dtype=torch.int32, device="cuda"), torch.arange(n, device="cuda")
+    out = [torch.empty_like(x) for _ in range(2)]
+    dw, lse = [torch.empty(D, device="cuda") for _ in range(2)], torch.empty(n, H, device="cuda")
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    plan = [i32(3), i32(1), i32(0, 0)[None].clone(), i32(1, 2), i32(2), 16, i32(0), i32(0, 0), i32(0), torch.zeros(1, dtype=torch.int64, device="cuda"), i32(0), i32(0)]
+    calls = [(lambda: lb.lory_qk_rope(x, x, pos, freq, q_out=out[0], k_out=out[1]), out, [x, pos, freq]),
+             (lambda: lb.lory_qk_rope_cache(x, x, x, pos, freq, kc, vc, slots, q_out=out[0], wq=w, wk=w), [kc, vc, out[0]], [x, slots, w]),
+             (lambda: lb.lory_qk_rope_bwd(x, x, x, x, pos, freq, w, w, dq=out[0], dk=out[1], dwq=dw[0], dwk=dw[1]), out + dw, [x, w]),
+             (lambda: lb.lory_paged_attn(x, kc, vc, table, pos, out=out[0], lse=lse), [out[0], lse], [x, kc, vc, table, pos]),
+             (lambda: lb.lory_kv_plan(*plan), plan[2:4] + plan[6:], [plan[0], plan[1], plan[4]])]
+    for i, (call, written, read) in enumerate(calls):
+        before = [t._version for t in written], [t._version for t in read]
+        call()
+        assert all(t._version > v for t, v in zip(written, before[0])), i
+        assert [t._version for t in read] == before[1], i
+    leaf = x.clone().requires_grad_()
+    h = leaf * 1.0
+    y = (h * h).sum()   # keeps h
+    lb.lory_qk_rope(h.detach(), x, pos, freq, q_out=h.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    with torch.inference_mode():
+        a = torch.empty_like(x)
+    lb.lory_qk_rope(x, x, pos, freq, q_out=a)   # a tensor without a version
+    assert torch.equal(a, lb.lory_qk_rope(x, x, pos, freq)[0])
