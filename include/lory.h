@@ -462,6 +462,9 @@ int lory_kv_plan(const lory_plan_shape *shape, const int32_t *lens, const int32_
  *      elements from row to row; lens [rows] int32
  * out: out [rows, q_heads, head_dim] (strided heads, may be q in place: same data
  *      and strides); lse [rows, q_heads] fp32 or NULL
+ * A call whose rows are all short under a table for long ones is divided for the
+ * long ones, as the lengths are on the device; a caller that knows a bound passes a
+ * smaller width (table_row stays).
  * Rows without a token (lens <= 0), and heads whose scores are all -inf, give 0
  * and lse -inf.  Lengths above width * page count as that.  A token whose page is
  * outside [0, pages) is left out.  What the cache holds behind a row's last token

@@ -490,7 +490,8 @@ def lory_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     """out [rows, q_heads, head_dim] = attention of one token per row, q, over the first lens[b] tokens that table [rows,
     width] finds in the caches [pages, kv_heads, page, head_dim]; lse [rows, q_heads] fp32 receives the log of
     the sum of exponentials.  scale is 1/sqrt(head_dim) unless given.  Row b of q goes with row b of table and lens: the
-    packed tokens of lory_kv_plan are other rows once one has ended or adds nothing.  Builds no graph."""
+    packed tokens of lory_kv_plan are other rows once one has ended or adds nothing.  table[:, :w] may be faster where no row
+    has more than w pages.  Builds no graph."""
     status, out = _native().paged_attn(q, k_cache, v_cache, table, lens, scale, out, lse, workspace)
     _check(status, "lory_paged_attn")
     return out

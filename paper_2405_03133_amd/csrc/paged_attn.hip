@@ -1,6 +1,7 @@
 // Attention of one new token per row over a paged key-value cache (lory_paged_attn).
 //
-// Bound by the bytes of the cache: every key and value is read once, for all query heads that share it.
+// Bound by the bytes of the cache: every key and value is read once for up to 16 query heads that share it, and again for
+// every 16 more.
 //
 // Work.  A unit is kTile keys of one key-value head of one row (of up to 16 of its query heads).  Short rows are a workgroup
 // each, or every row is cut into the same number of ranges; else the units of all rows and heads, in order, are cut into as
@@ -17,12 +18,13 @@
 // read whole by 16 lanes; lane i holds dims nt i .. nt i + nt - 1 of eight keys, and a v_perm per pair of keys gives the operand of
 // one matrix instruction per dim: row i of output tile t is dim nt i + t.  fp32 needs no transposition (one key per lane and instruction).
 // The probabilities go in as two bf16 terms (p = hi + lo, error 2^-16): one alone would round every weight of the sum to
-// 2^-8, and the matrix cores wait for memory anyway.
+// 2^-8, and the matrix cores wait for memory anyway.  An infinite value would be NaN with the second term; a wavefront whose
+// sums are not finite takes its keys again and leaves it out there (the check costs 0.1 to 0.3 us a call).
 //
 // Pages: the lane that owns a key looks its page up two steps ahead; the others fetch the row by a lane permute.
 //
-// Measured: four rows of 50000 to 131072 tokens, 32 query heads on 8, heads of 128, bf16: 216 us + 5.8 for the join, 6.6 TB/s
-// (a pass that only reads reaches 6.7); 48 rows of 1 to 9000 tokens 22.5 + 5.0 us, 4.6 TB/s; HBM traffic is the cache's
+// Measured: four rows of 50000 to 131072 tokens, 32 query heads on 8, heads of 128, bf16: 216 us + 5.8 for the join, 6.5 TB/s
+// (a pass that only reads reaches 6.7); 48 rows of 1 to 9000 tokens 22.8 + 5.2 us, 4.5 TB/s; HBM traffic is the cache's
 // bytes and 1 MB of pieces.  One CU takes in about 60 bytes per ns however many loads are under way (a second step in flight,
 // 16 wavefronts instead of eight or steps of 16 keys change nothing), so a short row costs 4 us and its bytes at that
 // rate.  Joining in the workgroup that finishes last instead of a second launch was tried: with fences between the XCDs
@@ -75,6 +77,11 @@ struct Args {
 // other layers want their share) when it is read again: from 64 MB on.  us with and without: four rows of 50000 to
 // 131072 tokens 220 / 246, 16 rows of 500 to 3000, 16 heads of 128 36.6 / 42, a ragged batch of 103 MB 28.0 / 30.3; 25 MB that
 // were read just before 10.1 / 9.0.  Keys are not: their lines are read by two instructions each (37.8 there).
+// The size is that of all pages, a sign of what else the program reads, and not what the call can reach: rows of 1000 tokens, 8 heads
+// of 128, in pages spread over 6 GB, read in turn with seven like calls 24 MB 12.1 / 11.9, 48 MB 17.1 / 19.1, 64 MB 19.1 / 21.5,
+// 128 MB 25.8 / 27.6; read again at once, which a program of several layers does not, 10.3 / 10.3, 16.0 / 14.7, 17.0 / 15.2, 22.9 / 22.6.
+// Nor does it matter that several workgroups read a value, for more than 16 query heads on a key-value head: 164 MB, 32 on one
+// 48.8 / 50.7, 64 on one 69.4 / 68.9, 123 MB, 128 on one 87.8 / 87.5 (called again at once 48.0 / 40.7, 67.8 / 58.6, 86.3 / 79.3).
 constexpr long kStreamBytes = 64l << 20;
 
 template <bool STREAM, typename V> __device__ __forceinline__ V load_value(const char *p)
@@ -387,7 +394,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             if (more) W::load_k(x, a.k, max(row, 0), a.D, i, c);
 
             // rounded before the maximum is taken off: equal scores of any size stay equal (a fused product would not); to
-            // base 2 only then, so that a score counts as long as fp32 holds it
+            // base 2 only then, so that a score counts as long as fp32 holds it and its product
 #pragma unroll
             for (int n = 0; n < NS; ++n) s[n] *= a.scale;
             if (valid != paged::all_keys(KEYS)) {
@@ -627,8 +634,8 @@ struct Plan {
 //    behind where all rows are long and ahead where few are: 200 rows of 2048 42 / 50; 800 heads of 64 over 100 to 4000
 //    tokens 62 / 52);
 //  - every row cut alike where the ranges fill the chip once at most and the longest is short, so that it does not matter whose
-//    row is long (28 heads of up to 3001 tokens, fp32: 18.1 us, 20.4 with ranges over all rows; with longer ranges a
-//    ragged batch of 48 rows takes 46 us against 31);
+//    row is long (28 heads of up to 3001 tokens, fp32: 18.1 us, 20.4 with ranges over all rows, both before full steps went
+//    without masks; with longer ranges a ragged batch of 48 rows takes 46 us against 31);
 //  - else equal ranges over all rows, which costs the sums over their lengths.
 Plan plan(const lory_paged_shape &s)
 {

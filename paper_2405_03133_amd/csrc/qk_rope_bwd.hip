@@ -8,7 +8,7 @@
 // 128 registers, four wavefronts per SIMD and 1024 workgroups, all resident at once: with 141 registers a quarter of them
 // waited for a second round (99 us against 79 for 16384 tokens of 32 heads of 128, bf16).  Workgroups of eight or 16 wavefronts leave
 // fewer rows to add but measured the same or slower (79.6, 86).
-// Measured: those 16384 tokens 73.4 us, 5.5 TB/s, and 4.6 us for the rows; 2999 fp32 tokens of 24 + 8 heads of 64 16.6 + 3.9 us.
+// Measured: those 16384 tokens 73.7 us, 5.5 TB/s, and 4.5 us for the rows; 2999 fp32 tokens of 24 + 8 heads of 64 16.7 + 3.8 us.
 #include "qk_rope.h"
 #include "qk_rope_plan.h"
 
