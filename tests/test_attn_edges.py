@@ -97,6 +97,61 @@ def test_generation_snippet_of_the_readme_with_a_row_that_has_ended():
     assert (s["out"][3:] == 0).all()   # places without a token
 
 
+def test_generation_snippet_of_the_readme_in_a_graph():
+    """Steps in which rows end at random, captured once and replayed with the program's own work in between: every replay against
+    the same step run eagerly, and every live row against 64 bits with its own query."""
+    text = open(os.path.join(ROOT, "README.md")).read()
+    code = compile(re.search(r"^Generation:.*?```python\n(.*?)```", text, re.S | re.M).group(1), "README.md", "exec")
+    B, W, page, F, Hq, Hkv, D = 6, 4, 8, 40, 4, 2, 64
+    g, rs = gen(41), np.random.RandomState(41)
+    i32 = lambda a: torch.tensor(np.asarray(a).tolist(), dtype=torch.int32, device="cuda")
+    wq, wk = 1 + rnd(g, D) / 4, 1 + rnd(g, D) / 4
+
+    def fresh():
+        qkv = torch.zeros(B, (Hq + 2 * Hkv) * D, device="cuda")
+        q, k, v = (x.unflatten(1, (-1, D)) for x in qkv.split([Hq * D, Hkv * D, Hkv * D], 1))
+        kc, vc = (torch.zeros(F, Hkv, page, D, device="cuda") for _ in range(2))
+        return dict(torch=torch, lb=lb, lens=i32([0] * B), add=i32([0] * B), table=i32(np.full((B, W), -1)), free=i32(range(F)), count=i32([F]),
+                    page=page, lens_new=i32([0] * B), cu=i32([0] * (B + 1)), positions=i32([0] * B),
+                    slots=torch.zeros(B, dtype=torch.int64, device="cuda"), count_new=i32([0]), status=i32([0]), q=q, k=k, v=v, freq=freqs(D),
+                    wq=wq, wk=wk, k_cache=kc, v_cache=vc), qkv
+
+    def step(s, q):
+        s["q"] = q
+        exec(code, s)
+        s["lens"].copy_(s["lens_new"])
+        s["count"].copy_(s["count_new"])
+
+    (eager, eager_qkv), (captured, captured_qkv) = fresh(), fresh()
+    eager_q, captured_q = eager["q"], captured["q"]
+    step(fresh()[0], eager_q.clone())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(captured, captured_q)
+    ended = 0
+    for i in range(20):
+        add = np.where(rs.rand(B) < 0.2, -1, np.where(rs.rand(B) < 0.2, 0, 1))
+        qkv = rnd(g, B, (Hq + 2 * Hkv) * D)
+        for s, x in ((eager, eager_qkv), (captured, captured_qkv)):
+            s["add"].copy_(i32(add))
+            x.copy_(qkv)
+        step(eager, eager_q)
+        graph.replay()
+        junk = torch.randn(1000, 1000, device="cuda")
+        (junk @ junk).sum().item()
+        for n in ("lens", "count", "table", "free", "cu", "positions", "slots", "status", "k_cache", "v_cache", "q", "out"):
+            assert torch.equal(captured[n], eager[n]), (i, n)
+        assert eager["status"].item() == 0
+        lens, live = eager["lens"].tolist(), [b for b in range(B) if add[b] > 0]
+        ended += (add < 0).sum()
+        for t, b in enumerate(live):
+            y, row, n = eager["q"][t:t + 1], eager["table"][b:b + 1], i32([lens[b]])
+            lse = torch.empty(1, Hq, device="cuda")
+            lb.lory_paged_attn(y, eager["k_cache"], eager["v_cache"], row, n, lse=lse)
+            check_attention(f"step {i} row {b}", eager["out"][t:t + 1], lse, y, eager["k_cache"], eager["v_cache"], row, n)
+    assert ended > 5
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens,Hq,Hkv,D,page", [([1, 37, 200], 2, 1, 64, 16), ([1, 130, 9], 17, 1, 40, 8), ([5000, 1, 64], 8, 2, 128, 16),
                                                 ([1, 300], 4, 2, 256, 16), ([333, 4000], 20, 4, 80, 24)])
