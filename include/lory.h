@@ -488,6 +488,108 @@ int lory_paged_attn(const lory_paged_shape *shape, const lory_heads *q, const vo
                     const int32_t *table, const int32_t *lens, const lory_heads *out, float *lse,
                     void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Several continuations of one prompt (beam search, parallel samples): which ones
+ * go on, the cache rows that go on from other rows, and the attention of rows
+ * that have their first tokens in common.  Rows of a request are neighbours: row
+ * request * beams + beam.  With prompt-only routing all rows of a request have
+ * the same merged parameters: their tokens are one sequence's of lory_dense_ffn_fwd.
+ *
+ * The k best continuations of every request over its beams and the vocabulary:
+ *   z[b][v] = score[b] + (x[b][v] - log sum_u exp x[b][u]),   x = logits[request * beams + b]
+ * in descending order, equal ones by beam and then by token.
+ * in:  logits [requests * beams, vocab] (dtype, aligned to it), `row` elements
+ *      from row to row; score [requests, beams] fp32, -inf for a beam that has ended
+ * out: score_out [requests, k] fp32, z; token [requests, k], v; parent [requests, k],
+ *      the row request * beams + b.  A z of -inf or NaN is no candidate, so a logit of
+ *      -inf bars its token, and a beam with a logit of NaN or +inf has none.  Where a request has
+ *      fewer than k candidates the last places have score -inf, token -1, parent -1.
+ * The order is that of z in fp64 (sums over a row: fp32 in chunks of 64 logits,
+ * fp64 over them); score_out is rounded once.
+ * 1 <= beams <= 64, 1 <= k <= 64, 1 <= vocab <= 500000, requests * beams <= 2^20.
+ * No output may overlap another array.
+ * workspace: lory_beam_select_workspace_bytes(shape); contents undefined before
+ * and after a call.
+ */
+typedef struct {
+    int32_t requests, beams, vocab, k;
+    int32_t dtype;
+    int64_t row;
+} lory_beam_shape;
+int lory_beam_select_workspace_bytes(const lory_beam_shape *shape, size_t *bytes_out);
+int lory_beam_select(const lory_beam_shape *shape, const void *logits, const float *score, float *score_out, int32_t *token,
+                     int32_t *parent, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rows of a paged cache that go on from other rows: row b of the new rows has the
+ * tokens of old row src[b] (src[b] < 0: none).  The same old row may go on as
+ * several new ones, or as none: so rows are forked, put in another order, closed up and
+ * ended in one call.  Whole pages are shared.  A last page that is partly filled stays with the
+ * lowest new row that has it; every other one takes a page from the stack of free pages, and
+ * `copies` says what goes there.  Pages that an old row has and no new row does come back.
+ *   free, count: as for lory_kv_plan.  Pages that come back go on top, by number;
+ *   then rows take theirs from the top, in order.
+ * in:     lens [old_rows]; src [rows]; table [old_rows, width], table_row elements
+ *         from row to row; count [1]
+ * in/out: free [free_size]
+ * out:    lens_new [rows]; table_new [rows, width], new_row elements from row to row (entries
+ *         behind a row's pages are not written); count_new [1]; copies [3, rows]: the
+ *         page that row b's tokens are copied from, the page that they go to, and how many
+ *         (-1, -1, 0 where nothing is copied), for lory_kv_copy; status [1]: 0, or the sum of
+ *           4  not enough free pages               8  more than free_size free pages
+ *          16  a length outside [0, width * page], a src above the old rows, a page
+ *              of a row outside [0, pages), or a count outside [0, free_size]
+ * With a status other than 0 free stays, lens_new = 0, count_new = count and nothing is to
+ * be copied; table_new may have been written.  The status stays on the device.
+ * A program keeps two sets of tables, lengths and counts and swaps them; a new token
+ * may be planned (lory_kv_plan) and stored once the copies have been made.  Rows that share pages end here, with no
+ * src that names them, and not by lory_kv_plan, which would give their pages back with the others' still in use.  To keep the
+ * pages of a prompt for later, keep a row of it.
+ * All arrays are int32.  No output may overlap another array (LORY_ERR_OVERLAP).
+ * Calling again with the same lens, src, table and count gives the same result.
+ * 1 <= page, pages, width, free_size; width * page < 2^31; rows, old_rows <= 2^20.
+ * workspace: lory_kv_fork_workspace_bytes(shape); contents undefined before and after a call.
+ */
+typedef struct {
+    int32_t old_rows, rows, width, page, pages, free_size;
+    int64_t table_row, new_row;
+} lory_fork_shape;
+int lory_kv_fork_workspace_bytes(const lory_fork_shape *shape, size_t *bytes_out);
+int lory_kv_fork(const lory_fork_shape *shape, const int32_t *lens, const int32_t *src, const int32_t *table, int32_t *free,
+                 const int32_t *count, int32_t *lens_new, int32_t *table_new, int32_t *count_new, int32_t *copies,
+                 int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Copies of pages inside a cache: the first copies[2][i] tokens (page at most) of page copies[0][i]
+ * go to page copies[1][i], for all heads, in keys and values, of every layer.
+ * in/out: k_cache, v_cache [layers, pages, kv_heads, page, head_dim] contiguous, 16-byte
+ *         aligned.  in: copies [3, n] int32
+ * Pairs with a page outside [0, pages), with both the same or with a count below 1 copy nothing.  A page
+ * that is written must be in one pair only: otherwise either result may stand.
+ * pages * kv_heads * page < 2^31, layers <= 32767, n <= 2^20; head_dim as above.
+ */
+typedef struct {
+    int32_t n, layers, pages, page, kv_heads, head_dim;
+    int32_t dtype;
+} lory_copy_shape;
+int lory_kv_copy(const lory_copy_shape *shape, void *k_cache, void *v_cache, const int32_t *copies, void *stream);
+
+/*
+ * lory_paged_attn for rows in `groups` groups of rows / groups neighbours each, whose
+ * first shared[g] tokens are the same: the keys and values of these tokens are read once for
+ * all rows of the group that have them.  Results are those of lory_paged_attn up to rounding.
+ * in:  shared [groups] int32: tokens of the cache that every row of group g with a length of shared[g] or
+ *      more has in common with the others.  They are read through the table of one of these rows: the
+ *      pages may be the same, or copies.  A shorter row (one that has no token, too) reads its own tokens
+ *      alone.  Values below 0 count as 0, above width * page as that.
+ * Everything else as for lory_paged_attn.  groups divides rows; rows / groups * (q_heads / kv_heads) < 2^30.
+ * workspace: lory_prefix_attn_workspace_bytes(shape, groups).
+ */
+int lory_prefix_attn_workspace_bytes(const lory_paged_shape *shape, int32_t groups, size_t *bytes_out);
+int lory_prefix_attn(const lory_paged_shape *shape, int32_t groups, const lory_heads *q, const void *k_cache, const void *v_cache,
+                     const int32_t *table, const int32_t *lens, const int32_t *shared, const lory_heads *out, float *lse,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,7 +31,8 @@ EXPORTS = ("lory_status_string", "lory_version", "lory_set_slab_budget", "lory_s
            "lory_route_bwd", "lory_merged_ffn_fwd", "lory_merged_ffn_bwd", "lory_prompt_merge",
            "lory_dense_ffn_fwd", "lory_dense_ffn_fwd_static", "lory_qk_rope", "lory_qk_rope_cache",
            "lory_qk_rope_workspace_bytes", "lory_qk_rope_bwd", "lory_kv_plan", "lory_paged_attn_workspace_bytes",
-           "lory_paged_attn")
+           "lory_paged_attn", "lory_beam_select_workspace_bytes", "lory_beam_select", "lory_kv_fork_workspace_bytes",
+           "lory_kv_fork", "lory_kv_copy", "lory_prefix_attn_workspace_bytes", "lory_prefix_attn")
 
 
 class LoryShape(ctypes.Structure):
@@ -65,6 +66,22 @@ class LoryPagedShape(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("pages", ctypes.c_int32), ("page", ctypes.c_int32),
                 ("width", ctypes.c_int32), ("dtype", ctypes.c_int32), ("table_row", ctypes.c_int64),
                 ("scale", ctypes.c_float)]
+
+
+class LoryBeamShape(ctypes.Structure):
+    _fields_ = [("requests", ctypes.c_int32), ("beams", ctypes.c_int32), ("vocab", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("row", ctypes.c_int64)]
+
+
+class LoryForkShape(ctypes.Structure):
+    _fields_ = [("old_rows", ctypes.c_int32), ("rows", ctypes.c_int32), ("width", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("pages", ctypes.c_int32), ("free_size", ctypes.c_int32), ("table_row", ctypes.c_int64),
+                ("new_row", ctypes.c_int64)]
+
+
+class LoryCopyShape(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("layers", ctypes.c_int32), ("pages", ctypes.c_int32), ("page", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 class LoryError(RuntimeError):
@@ -132,6 +149,20 @@ def lib() -> ctypes.CDLL:
         L.lory_paged_attn_workspace_bytes.restype = ci
         L.lory_paged_attn.argtypes = [ap, hp, vp, vp, vp, vp, hp, vp, vp, sz, vp]
         L.lory_paged_attn.restype = ci
+        L.lory_beam_select_workspace_bytes.argtypes = [ctypes.POINTER(LoryBeamShape), ctypes.POINTER(sz)]
+        L.lory_beam_select_workspace_bytes.restype = ci
+        L.lory_beam_select.argtypes = [ctypes.POINTER(LoryBeamShape)] + [vp] * 6 + [sz, vp]
+        L.lory_beam_select.restype = ci
+        L.lory_kv_fork_workspace_bytes.argtypes = [ctypes.POINTER(LoryForkShape), ctypes.POINTER(sz)]
+        L.lory_kv_fork_workspace_bytes.restype = ci
+        L.lory_kv_fork.argtypes = [ctypes.POINTER(LoryForkShape)] + [vp] * 11 + [sz, vp]
+        L.lory_kv_fork.restype = ci
+        L.lory_kv_copy.argtypes = [ctypes.POINTER(LoryCopyShape)] + [vp] * 4
+        L.lory_kv_copy.restype = ci
+        L.lory_prefix_attn_workspace_bytes.argtypes = [ap, ctypes.c_int32, ctypes.POINTER(sz)]
+        L.lory_prefix_attn_workspace_bytes.restype = ci
+        L.lory_prefix_attn.argtypes = [ap, ctypes.c_int32, hp] + [vp] * 5 + [hp, vp, vp, sz, vp]
+        L.lory_prefix_attn.restype = ci
         _lib = L
     return _lib
 
@@ -494,4 +525,88 @@ def lory_paged_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     has more than w pages.  Builds no graph."""
     status, out = _native().paged_attn(q, k_cache, v_cache, table, lens, scale, out, lse, workspace)
     _check(status, "lory_paged_attn")
+    return out
+
+
+# ---- several continuations of one prompt: selection, forked rows of the cache, a prefix that rows share
+
+
+def lory_beam_select_workspace_bytes(shape: LoryBeamShape) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().lory_beam_select_workspace_bytes(shape, ctypes.byref(out)), "lory_beam_select_workspace_bytes")
+    return out.value
+
+
+def alloc_beam_select_workspace(logits: torch.Tensor, score: torch.Tensor, k: int) -> torch.Tensor:
+    """Workspace of lory_beam_select for these shapes."""
+    R, K = score.shape
+    V = logits.shape[1]
+    n = lory_beam_select_workspace_bytes(LoryBeamShape(R, K, V, k, _dtype_code(logits.dtype), V))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=logits.device)
+
+
+def lory_beam_select(logits: torch.Tensor, score: torch.Tensor, k: int, score_out: Optional[torch.Tensor] = None,
+                     token: Optional[torch.Tensor] = None, parent: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """The k best continuations of every request by score + log softmax of logits: logits [requests * beams, vocab], score
+    [requests, beams] fp32 (-inf: the beam has ended).  Returns (score_out fp32, token, parent) [requests, k], best first; parent is a
+    row of logits (src of lory_kv_fork).  Where there are fewer than k: -inf, -1, -1.  Builds no graph."""
+    status, score_out, token, parent = _native().beam_select(logits, score, k, score_out, token, parent, workspace)
+    _check(status, "lory_beam_select")
+    return score_out, token, parent
+
+
+def lory_kv_fork_workspace_bytes(shape: LoryForkShape) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().lory_kv_fork_workspace_bytes(shape, ctypes.byref(out)), "lory_kv_fork_workspace_bytes")
+    return out.value
+
+
+def alloc_kv_fork_workspace(src: torch.Tensor, table: torch.Tensor, pages: int) -> torch.Tensor:
+    """Workspace of lory_kv_fork for these shapes and a pool of `pages`."""
+    old, width = table.shape
+    n = lory_kv_fork_workspace_bytes(LoryForkShape(old, src.shape[0], width, 1, pages, 1, width, width))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=table.device)
+
+
+def lory_kv_fork(lens: torch.Tensor, src: torch.Tensor, table: torch.Tensor, free: torch.Tensor, count: torch.Tensor, page: int,
+                 pages: int, lens_new: torch.Tensor, table_new: torch.Tensor, count_new: torch.Tensor, copies: torch.Tensor,
+                 status: torch.Tensor, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """New rows of a cache of `pages` pages, each with the tokens of old row src[b] (below 0: none): whole pages are shared, partly
+    filled ones get a page of their own and an entry in copies [3, rows] (for lory_kv_copy), and pages that no new row has come
+    back; all int32.  Returns status [1]: 0, or why nothing was done (include/lory.h)."""
+    _check(_native().kv_fork(lens, src, table, free, count, page, pages, lens_new, table_new, count_new, copies, status, workspace),
+           "lory_kv_fork")
+    return status
+
+
+def lory_kv_copy(k_cache: torch.Tensor, v_cache: torch.Tensor, copies: torch.Tensor) -> None:
+    """The first copies[2, i] tokens of page copies[0, i] go to page copies[1, i] of the caches [pages, kv_heads, page, head_dim] or
+    [layers, pages, kv_heads, page, head_dim]; pairs with a page outside of them copy nothing."""
+    _check(_native().kv_copy(k_cache, v_cache, copies), "lory_kv_copy")
+
+
+def lory_prefix_attn_workspace_bytes(shape: LoryPagedShape, groups: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().lory_prefix_attn_workspace_bytes(shape, groups, ctypes.byref(out)), "lory_prefix_attn_workspace_bytes")
+    return out.value
+
+
+def alloc_prefix_attn_workspace(q: torch.Tensor, k_cache: torch.Tensor, table: torch.Tensor, shared: torch.Tensor) -> torch.Tensor:
+    """Workspace of lory_prefix_attn for these shapes."""
+    B, Hq, D = q.shape
+    pages, Hkv, page, _ = k_cache.shape
+    width = table.shape[1]
+    n = lory_prefix_attn_workspace_bytes(LoryPagedShape(B, Hq, Hkv, D, pages, page, width, _dtype_code(q.dtype), width, 1.0),
+                                         shared.shape[0])
+    return torch.empty(n, dtype=torch.uint8, device=q.device)
+
+
+def lory_prefix_attn(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                     shared: torch.Tensor, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, scale: Optional[float] = None) -> torch.Tensor:
+    """lory_paged_attn for rows in groups of rows / len(shared) neighbours whose first shared[g] tokens are the same: these are read
+    once for all rows of a group.  Rows with fewer tokens than that read their own alone."""
+    status, out = _native().prefix_attn(q, k_cache, v_cache, table, lens, shared, scale, out, lse, workspace)
+    _check(status, "lory_prefix_attn")
     return out

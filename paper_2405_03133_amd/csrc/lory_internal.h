@@ -44,7 +44,7 @@ inline int launch_status()
 namespace prof {
 enum Class { kRoute = 0, kMerge, kGemmGU, kSwigluFwd, kGemmDown, kGemmDA, kSwigluBwd, kGemmDX, kGemmDWGU, kGemmDWD, kScatter,
              kDwReduce, kRouteBwd, kDenseSkinny, kFusedGU, kFusedDown, kFusedDA, kFusedDX, kFusedDW,
-             kQkRope, kQkRopeBwd, kKvPlan, kPagedAttn, kNumClasses };
+             kQkRope, kQkRopeBwd, kKvPlan, kPagedAttn, kBeamSelect, kKvFork, kKvCopy, kPrefixAttn, kNumClasses };
 bool enabled();
 int set_enabled(int on);
 int read(lory_kernel_stat *out, int max_out, int *n_out);
@@ -168,5 +168,19 @@ int kv_plan_launch(const lory_plan_shape &s, const int32_t *lens, const int32_t 
 size_t paged_attn_workspace_bytes(const lory_paged_shape &s);
 int paged_attn_launch(const lory_paged_shape &s, const lory_heads &q, const void *k_cache, const void *v_cache,
                       const int32_t *table, const int32_t *lens, const lory_heads &out, float *lse, void *ws, hipStream_t st);
+
+// ---- several continuations of one prompt (beam_select.hip, kv_fork.hip, prefix_attn.hip); arguments are checked
+size_t beam_select_workspace_bytes(const lory_beam_shape &s);
+int beam_select_launch(const lory_beam_shape &s, const void *logits, const float *score, float *score_out, int32_t *token,
+                       int32_t *parent, void *ws, hipStream_t st);
+size_t kv_fork_workspace_bytes(const lory_fork_shape &s);
+int kv_fork_launch(const lory_fork_shape &s, const int32_t *lens, const int32_t *src, const int32_t *table, int32_t *free,
+                   const int32_t *count, int32_t *lens_new, int32_t *table_new, int32_t *count_new, int32_t *copies,
+                   int32_t *status, void *ws, hipStream_t st);
+int kv_copy_launch(const lory_copy_shape &s, void *k_cache, void *v_cache, const int32_t *copies, hipStream_t st);
+size_t prefix_attn_workspace_bytes(const lory_paged_shape &s, int groups);
+int prefix_attn_launch(const lory_paged_shape &s, int groups, const lory_heads &q, const void *k_cache, const void *v_cache,
+                       const int32_t *table, const int32_t *lens, const int32_t *shared, const lory_heads &out, float *lse, void *ws,
+                       hipStream_t st);
 
 }  // namespace lory

@@ -114,13 +114,13 @@ struct Call {
         if (n > INT32_MAX) raise(PyExc_ValueError, "%s is too large", name);
         return (int)n;
     }
-    int32_t *table(int i, int64_t rows, int &width, int64_t &row)
+    int32_t *table(int i, int64_t rows, int &width, int64_t &row, const char *name = "table")
     {
-        const at::Tensor &t = tensor(i, "table");
+        const at::Tensor &t = tensor(i, name);
         if (t.scalar_type() != at::kInt || t.dim() != 2 || t.size(0) != rows || (t.size(1) > 1 && t.stride(1) != 1))
-            raise(PyExc_ValueError, "table must be int32 [%lld, width] with contiguous rows", (long long)rows);
-        on_gpu(t, "table");
-        width = size32(t.size(1), "table");
+            raise(PyExc_ValueError, "%s must be int32 [%lld, width] with contiguous rows", name, (long long)rows);
+        on_gpu(t, name);
+        width = size32(t.size(1), name);
         row = rows > 1 ? t.stride(0) : width;
         return (int32_t *)t.data_ptr();
     }
@@ -321,44 +321,171 @@ PyObject *kv_plan(Call &c)
     return PyLong_FromLong(c.done(lory_kv_plan(&s, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], slots, p[9], p[10], stream)));
 }
 
+// What the two attention calls share: q, k_cache, v_cache, table, lens at 0 to 4.
+struct Paged {
+    lory_paged_shape s = {};
+    lory_heads q;
+    const void *k, *v;
+    const int32_t *table, *lens;
+    int64_t B, Hq, D;
+
+    Paged(Call &c, PyObject *scale)
+    {
+        const at::Tensor &tq = c.tensor(0, "q");
+        s.dtype = c.dtype(tq, "q");
+        if (tq.dim() != 3) raise(PyExc_ValueError, "q must be [rows, heads, head_dim]");
+        B = tq.size(0), Hq = tq.size(1), D = tq.size(2);
+        q = c.heads(tq, B, Hq, D, "q");
+        const at::Tensor &kc = c.tensor(1, "k_cache");
+        const int64_t Hkv = kc.dim() == 4 ? kc.size(1) : -1;
+        s.pages = s.page = -1;
+        k = c.cache(1, Hkv, D, s.pages, s.page, "k_cache"), v = c.cache(2, Hkv, D, s.pages, s.page, "v_cache");
+        table = c.table(3, B, s.width, s.table_row), lens = c.ints(4, B, "lens");
+        s.rows = c.size32(B, "q");
+        s.q_heads = c.size32(Hq, "q");
+        s.kv_heads = c.size32(Hkv, "k_cache");
+        s.head_dim = c.size32(D, "q");
+        s.scale = scale == Py_None ? (float)(1.0 / std::sqrt((double)(D > 0 ? D : 1))) : (float)number(scale);
+    }
+    float *lse(Call &c, int i) const
+    {
+        if (c.none(i)) return nullptr;
+        const at::Tensor &t = c.tensor(i, "lse");
+        if (t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) != B || t.size(1) != Hq)
+            raise(PyExc_ValueError, "lse must be fp32 [%lld, %lld]", (long long)B, (long long)Hq);
+        return (float *)c.contiguous(t, "lse");
+    }
+};
+
+// The workspace that was given at i, or a new one of the size that `size` reports.
+template <typename Size> void *workspace_or_new(Call &c, int i, size_t &bytes, at::Tensor &own, const at::Tensor &like, const Size &size)
+{
+    void *ws = c.workspace(i, bytes);
+    if (c.none(i) && size(&bytes) == LORY_OK && bytes > 0) {
+        own = at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
+        ws = own.data_ptr();
+    }
+    return ws;
+}
+
 // q, k_cache, v_cache, table, lens, scale, out, lse, workspace
 PyObject *paged_attn(Call &c)
 {
+    const Paged p(c, c.args[5]);
     const at::Tensor &tq = c.tensor(0, "q");
-    lory_paged_shape s = {};
-    s.dtype = c.dtype(tq, "q");
-    if (tq.dim() != 3) raise(PyExc_ValueError, "q must be [rows, heads, head_dim]");
-    const int64_t B = tq.size(0), Hq = tq.size(1), D = tq.size(2);
-    const lory_heads q = c.heads(tq, B, Hq, D, "q");
-    const at::Tensor &kc = c.tensor(1, "k_cache");
-    const int64_t Hkv = kc.dim() == 4 ? kc.size(1) : -1;
-    s.pages = s.page = -1;
-    const void *k = c.cache(1, Hkv, D, s.pages, s.page, "k_cache"), *v = c.cache(2, Hkv, D, s.pages, s.page, "v_cache");
-    const int32_t *table = c.table(3, B, s.width, s.table_row), *lens = c.ints(4, B, "lens");
-    s.rows = c.size32(B, "q");
-    s.q_heads = c.size32(Hq, "q");
-    s.kv_heads = c.size32(Hkv, "k_cache");
-    s.head_dim = c.size32(D, "q");
-    s.scale = c.none(5) ? (float)(1.0 / std::sqrt((double)(D > 0 ? D : 1))) : (float)number(c.args[5]);
     const at::Tensor to = c.output(6, tq, "out");
-    const lory_heads out = c.heads(to, B, Hq, D, "out");
-    float *lse = nullptr;
-    if (!c.none(7)) {
-        const at::Tensor &t = c.tensor(7, "lse");
-        if (t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) != B || t.size(1) != Hq)
-            raise(PyExc_ValueError, "lse must be fp32 [%lld, %lld]", (long long)B, (long long)Hq);
-        lse = (float *)c.contiguous(t, "lse");
-    }
+    const lory_heads out = c.heads(to, p.B, p.Hq, p.D, "out");
+    float *lse = p.lse(c, 7);
     size_t bytes = 0;
-    void *ws = c.workspace(8, bytes);
     at::Tensor own;
-    if (c.none(8) && lory_paged_attn_workspace_bytes(&s, &bytes) == LORY_OK) {
-        own = at::empty({(int64_t)bytes}, tq.options().dtype(at::kByte));
-        ws = own.data_ptr();
-    }
+    void *ws = workspace_or_new(c, 8, bytes, own, tq, [&](size_t *n) { return lory_paged_attn_workspace_bytes(&p.s, n); });
     void *stream = c.stream();
     c.writes({6, 7});
-    return result(c.done(lory_paged_attn(&s, &q, k, v, table, lens, &out, lse, ws, bytes, stream)), {to});
+    return result(c.done(lory_paged_attn(&p.s, &p.q, p.k, p.v, p.table, p.lens, &out, lse, ws, bytes, stream)), {to});
+}
+
+// q, k_cache, v_cache, table, lens, shared, scale, out, lse, workspace
+PyObject *prefix_attn(Call &c)
+{
+    const Paged p(c, c.args[6]);
+    const at::Tensor &tq = c.tensor(0, "q"), &ts = c.tensor(5, "shared");
+    const int64_t G = ts.dim() == 1 ? ts.size(0) : -1;
+    const int32_t *shared = c.ints(5, G, "shared");
+    const int groups = c.size32(G, "shared");
+    if (groups > 0 ? p.B % groups != 0 || p.B == 0 : p.B != 0)
+        raise(PyExc_ValueError, "shared must have a value for every group of neighbouring rows: %lld rows, %d groups", (long long)p.B, groups);
+    const at::Tensor to = c.output(7, tq, "out");
+    const lory_heads out = c.heads(to, p.B, p.Hq, p.D, "out");
+    float *lse = p.lse(c, 8);
+    size_t bytes = 0;
+    at::Tensor own;
+    void *ws = workspace_or_new(c, 9, bytes, own, tq, [&](size_t *n) { return lory_prefix_attn_workspace_bytes(&p.s, groups, n); });
+    void *stream = c.stream();
+    c.writes({7, 8});
+    return result(c.done(lory_prefix_attn(&p.s, groups, &p.q, p.k, p.v, p.table, p.lens, shared, &out, lse, ws, bytes, stream)), {to});
+}
+
+// logits, score, k, score_out, token, parent, workspace
+PyObject *beam_select(Call &c)
+{
+    const at::Tensor &x = c.tensor(0, "logits"), &score = c.tensor(1, "score");
+    lory_beam_shape s = {};
+    s.dtype = c.dtype(x, "logits");
+    if (score.scalar_type() != at::kFloat || score.dim() != 2) raise(PyExc_ValueError, "score must be fp32 [requests, beams]");
+    const int64_t R = score.size(0), K = score.size(1);
+    const float *sc = (const float *)c.contiguous(score, "score");
+    if (x.dim() != 2 || x.size(0) != R * K || (x.size(1) > 1 && x.stride(1) != 1))
+        raise(PyExc_ValueError, "logits must be [%lld, vocab] with contiguous rows", (long long)(R * K));
+    c.on_gpu(x, "logits");
+    s.requests = c.size32(R, "score");
+    s.beams = c.size32(K, "score");
+    s.vocab = c.size32(x.size(1), "logits");
+    s.k = whole(c.args[2], "k");
+    s.row = R * K > 1 ? x.stride(0) : s.vocab;
+    at::Tensor out[3];
+    void *p[3];
+    const char *const names[3] = {"score_out", "token", "parent"};
+    for (int i = 0; i < 3; ++i) {
+        const at::ScalarType type = i ? at::kInt : at::kFloat;
+        out[i] = c.none(3 + i) ? at::empty({R, s.k > 0 ? s.k : 0}, score.options().dtype(type)) : c.tensor(3 + i, names[i]);
+        if (out[i].scalar_type() != type || out[i].dim() != 2 || out[i].size(0) != R || out[i].size(1) != s.k)
+            if (s.k > 0) raise(PyExc_ValueError, "%s must be %s [%lld, %d]", names[i], c10::toString(type), (long long)R, s.k);
+        p[i] = c.contiguous(out[i], names[i]);
+    }
+    size_t bytes = 0;
+    at::Tensor own;
+    void *ws = workspace_or_new(c, 6, bytes, own, x, [&](size_t *n) { return lory_beam_select_workspace_bytes(&s, n); });
+    void *stream = c.stream();
+    c.writes({3, 4, 5});
+    return result(c.done(lory_beam_select(&s, x.data_ptr(), sc, (float *)p[0], (int32_t *)p[1], (int32_t *)p[2], ws, bytes, stream)),
+                  {out[0], out[1], out[2]});
+}
+
+// lens, src, table, free, count, page, pages, lens_new, table_new, count_new, copies, status, workspace
+PyObject *kv_fork(Call &c)
+{
+    const at::Tensor &lens = c.tensor(0, "lens"), &src = c.tensor(1, "src"), &free = c.tensor(3, "free"), &copies = c.tensor(10, "copies");
+    const int64_t old = lens.dim() == 1 ? lens.size(0) : -1, N = src.dim() == 1 ? src.size(0) : -1, F = free.dim() == 1 ? free.size(0) : -1;
+    lory_fork_shape s = {c.size32(old, "lens"), c.size32(N, "src"), 0, whole(c.args[5], "page"), whole(c.args[6], "pages"),
+                         c.size32(F, "free"), 0, 0};
+    int32_t *p[9] = {c.ints(0, old, "lens"), c.ints(1, N, "src"), c.table(2, old, s.width, s.table_row), c.ints(3, F, "free"),
+                     c.ints(4, 1, "count"), c.ints(7, N, "lens_new"), nullptr, c.ints(9, 1, "count_new"), c.ints(11, 1, "status")};
+    int width = 0;
+    p[6] = c.table(8, N, width, s.new_row, "table_new");
+    if (width != s.width) raise(PyExc_ValueError, "table_new must have the width of table, %d", s.width);
+    if (copies.scalar_type() != at::kInt || copies.dim() != 2 || copies.size(0) != 3 || copies.size(1) != N)
+        raise(PyExc_ValueError, "copies must be int32 [3, %lld]", (long long)N);
+    int32_t *pc = (int32_t *)c.contiguous(copies, "copies");
+    size_t bytes = 0;
+    at::Tensor own;
+    void *ws = workspace_or_new(c, 12, bytes, own, lens, [&](size_t *n) { return lory_kv_fork_workspace_bytes(&s, n); });
+    void *stream = c.stream();
+    c.writes({3, 7, 8, 9, 10, 11});
+    return PyLong_FromLong(c.done(lory_kv_fork(&s, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], pc, p[8], ws, bytes, stream)));
+}
+
+// k_cache, v_cache, copies
+PyObject *kv_copy(Call &c)
+{
+    const at::Tensor &k = c.tensor(0, "k_cache"), &v = c.tensor(1, "v_cache"), &copies = c.tensor(2, "copies");
+    lory_copy_shape s = {};
+    s.dtype = c.dtype(k, "k_cache");
+    c.of_type(v, c.type, "v_cache");
+    const int64_t d = k.dim();
+    if ((d != 4 && d != 5) || v.sizes() != k.sizes())
+        raise(PyExc_ValueError, "k_cache and v_cache must be [pages, heads, page, head_dim], or [layers, ...] of that");
+    void *pk = c.contiguous(k, "k_cache"), *pv = c.contiguous(v, "v_cache");
+    if (copies.scalar_type() != at::kInt || copies.dim() != 2 || copies.size(0) != 3) raise(PyExc_ValueError, "copies must be int32 [3, n]");
+    const int32_t *pc = (const int32_t *)c.contiguous(copies, "copies");
+    s.n = c.size32(copies.size(1), "copies");
+    s.layers = d == 5 ? c.size32(k.size(0), "k_cache") : 1;
+    s.pages = c.size32(k.size(d - 4), "k_cache");
+    s.kv_heads = c.size32(k.size(d - 3), "k_cache");
+    s.page = c.size32(k.size(d - 2), "k_cache");
+    s.head_dim = c.size32(k.size(d - 1), "k_cache");
+    void *stream = c.stream();
+    c.writes({0, 1});
+    return PyLong_FromLong(c.done(lory_kv_copy(&s, pk, pv, pc, stream)));
 }
 
 PyMethodDef methods[] = {
@@ -367,6 +494,10 @@ PyMethodDef methods[] = {
     {"qk_rope_bwd", (PyCFunction)(void (*)(void))entry<qk_rope_bwd, 15>, METH_FASTCALL, nullptr},
     {"kv_plan", (PyCFunction)(void (*)(void))entry<kv_plan, 12>, METH_FASTCALL, nullptr},
     {"paged_attn", (PyCFunction)(void (*)(void))entry<paged_attn, 9>, METH_FASTCALL, nullptr},
+    {"prefix_attn", (PyCFunction)(void (*)(void))entry<prefix_attn, 10>, METH_FASTCALL, nullptr},
+    {"beam_select", (PyCFunction)(void (*)(void))entry<beam_select, 7>, METH_FASTCALL, nullptr},
+    {"kv_fork", (PyCFunction)(void (*)(void))entry<kv_fork, 13>, METH_FASTCALL, nullptr},
+    {"kv_copy", (PyCFunction)(void (*)(void))entry<kv_copy, 3>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

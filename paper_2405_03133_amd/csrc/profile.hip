@@ -32,7 +32,8 @@ const char *const kNames[kNumClasses] = {"route",     "merge",     "gemm_gate_up
                                          "gemm_dA",   "swiglu_bwd", "gemm_dX",   "gemm_dW_gate_up",
                                          "gemm_dW_down", "scatter_dots", "dw_reduce", "route_bwd", "dense_skinny",
                                          "fused_gate_up", "fused_down", "fused_dA", "fused_dX", "fused_dW_dots",
-                                         "qk_rope", "qk_rope_bwd", "kv_plan", "paged_attn"};
+                                         "qk_rope", "qk_rope_bwd", "kv_plan", "paged_attn",
+                                         "beam_select", "kv_fork", "kv_copy", "prefix_attn"};
 
 // Events are created when timing is switched on (and by lory_profile_read, which returns
 // them to the pool), never inside a launch: a launch only takes events from the pool and
