@@ -497,16 +497,16 @@ int lory_paged_attn(const lory_paged_shape *shape, const lory_heads *q, const vo
  *
  * The k best continuations of every request over its beams and the vocabulary:
  *   z[b][v] = score[b] + (x[b][v] - log sum_u exp x[b][u]),   x = logits[request * beams + b]
- * in descending order, equal ones by beam and then by token.
+ * in descending order, equal ones by beam, in a beam by logit, then by token.
  * in:  logits [requests * beams, vocab] (dtype, aligned to it), `row` elements
  *      from row to row; score [requests, beams] fp32, -inf for a beam that has ended
  * out: score_out [requests, k] fp32, z; token [requests, k], v; parent [requests, k],
  *      the row request * beams + b.  A z of -inf or NaN is no candidate, so a logit of
  *      -inf bars its token, and a beam with a logit of NaN or +inf has none.  Where a request has
  *      fewer than k candidates the last places have score -inf, token -1, parent -1.
- * The order is that of z in fp64 (sums over a row: fp32 in chunks of 64 logits,
+ * The order is that of z in fp64 (sums over a row: fp32 in groups of 32 logits,
  * fp64 over them); score_out is rounded once.
- * 1 <= beams <= 64, 1 <= k <= 64, 1 <= vocab <= 500000, requests * beams <= 2^20.
+ * 1 <= beams <= 64, 1 <= k <= 64, 1 <= vocab <= 2^24, requests * beams <= 2^20.
  * No output may overlap another array.
  * workspace: lory_beam_select_workspace_bytes(shape); contents undefined before
  * and after a call.

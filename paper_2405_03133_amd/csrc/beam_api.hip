@@ -11,7 +11,7 @@ int check_beam(const lory_beam_shape *s)
     if (!s) return LORY_ERR_NULL;
     if (!esize_of(s->dtype)) return LORY_ERR_DTYPE;
     if (s->requests < 0 || s->beams <= 0 || s->beams > 64 || (long)s->requests * s->beams > (1 << 20) || s->vocab <= 0 ||
-        s->vocab > 500000 || s->k <= 0 || s->k > 64 || s->row < s->vocab || s->row > kMaxStride)
+        s->vocab > (1 << 24) || s->k <= 0 || s->k > 64 || s->row < s->vocab || s->row > kMaxStride)
         return LORY_ERR_SHAPE;
     return LORY_OK;
 }
