@@ -582,7 +582,8 @@ int lory_kv_copy(const lory_copy_shape *shape, void *k_cache, void *v_cache, con
  *      more has in common with the others.  They are read through the table of one of these rows: the
  *      pages may be the same, or copies.  A shorter row (one that has no token, too) reads its own tokens
  *      alone.  Values below 0 count as 0, above width * page as that.
- * Everything else as for lory_paged_attn.  groups divides rows; rows / groups * (q_heads / kv_heads) < 2^30.
+ * Everything else as for lory_paged_attn.  groups divides rows; rows / groups * (q_heads / kv_heads) < 2^30,
+ * rows * (width * page / 64 + 4) < 2^31.
  * workspace: lory_prefix_attn_workspace_bytes(shape, groups).
  */
 int lory_prefix_attn_workspace_bytes(const lory_paged_shape *shape, int32_t groups, size_t *bytes_out);

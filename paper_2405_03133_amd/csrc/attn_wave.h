@@ -43,7 +43,7 @@ __device__ __forceinline__ float xor_sum(float v)
     return v + __shfl_xor(v, 32, 64);
 }
 
-// One key-value head for one wavefront: the operands of the queries, and the outputs.
+// One key-value head for one wavefront: operands of keys, values and queries (16 of them), and the outputs.
 // DP: head_dim rounded up to 64, 128 or 256.  PAD: head_dim < DP (pieces behind it are zeros that nothing loads).
 template <typename T, int DP, bool PAD, int NQ = 1> struct Wave;
 
@@ -56,19 +56,20 @@ template <int DP, bool PAD, int NQ> struct Wave<__hip_bfloat16, DP, PAD, NQ> {
         u32x4 k[2][KS];
         uint32_t v[8][VL][VW / 2];
     };
-    bf16x8 q[NQ][KS];
+    typedef bf16x8 Query[KS];
+    Query q[NQ];
     f32x4 o[NQ][NT];
 
     // dim of row i of output tile t
     static __device__ int dim(int t, int i) { return (t / VW) * 16 * VW + VW * i + t % VW; }
 
-    __device__ void load_q(int b, const char *p, int D, int c, bool on)
+    __device__ static void load_q(Query &q, const char *p, int D, int c, bool on)
     {
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
             u32x4 r = {0, 0, 0, 0};
             if (on && (!PAD || (4 * s + c) * 8 < D)) r = *reinterpret_cast<const u32x4 *>(p + (4 * s + c) * 16);
-            q[b][s] = __builtin_bit_cast(bf16x8, r);
+            q[s] = __builtin_bit_cast(bf16x8, r);
         }
     }
     // row: of the lane's own key of the step (lane & 31)
@@ -107,15 +108,15 @@ template <int DP, bool PAD, int NQ> struct Wave<__hip_bfloat16, DP, PAD, NQ> {
             }
         }
     }
-    // s[n]: score of the lane's query of block b with key (n / 4) * 16 + 4c + n % 4
-    __device__ void scores(int b, const Keys &x, float (&s)[8])
+    // s[n]: score of the lane's query with key (n / 4) * 16 + 4c + n % 4
+    __device__ static void scores(const bf16x8 (&q)[KS], const Keys &x, float (&s)[8])
     {
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int t = 0; t < KS; ++t)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[kt][t]), q[b][t], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x.k[kt][t]), q[t], acc, 0, 0, 0);
 #pragma unroll
             for (int r = 0; r < 4; ++r) s[kt * 4 + r] = acc[r];
         }
@@ -190,17 +191,18 @@ template <int DP, bool PAD, int NQ> struct Wave<float, DP, PAD, NQ> {
         f32x4 k[KS];
         f32x4 v[4][VL];
     };
-    f32x4 q[NQ][KS];
+    typedef f32x4 Query[KS];
+    Query q[NQ];
     f32x4 o[NQ][NT];
 
     static __device__ int dim(int t, int i) { return (t / 4) * 64 + 4 * i + t % 4; }
 
-    __device__ void load_q(int b, const char *p, int D, int c, bool on)
+    __device__ static void load_q(Query &q, const char *p, int D, int c, bool on)
     {
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            q[b][s] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (on && (!PAD || (4 * s + c) * 4 < D)) q[b][s] = *reinterpret_cast<const f32x4 *>(p + (4 * s + c) * 16);
+            q[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (on && (!PAD || (4 * s + c) * 4 < D)) q[s] = *reinterpret_cast<const f32x4 *>(p + (4 * s + c) * 16);
         }
     }
     __device__ static void load_k(Keys &x, const char *base, int row, int D, int i, int c)
@@ -226,13 +228,13 @@ template <int DP, bool PAD, int NQ> struct Wave<float, DP, PAD, NQ> {
             }
         }
     }
-    __device__ void scores(int b, const Keys &x, float (&s)[4])
+    __device__ static void scores(const f32x4 (&q)[KS], const Keys &x, float (&s)[4])
     {
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < KS; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.k[t][e], q[b][t][e], acc, 0, 0, 0);
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(x.k[t][e], q[t][e], acc, 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 4; ++r) s[r] = acc[r];
     }

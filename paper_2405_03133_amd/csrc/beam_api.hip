@@ -31,6 +31,8 @@ int check_prefix(const lory_paged_shape *s, int groups)
     const int rc = check_paged(s);
     if (rc != LORY_OK) return rc;
     if (groups < 0 || (s->rows > 0 && groups == 0) || groups > s->rows || (groups > 0 && s->rows % groups != 0)) return LORY_ERR_SHAPE;
+    // the kernel counts units of 64 keys, and two more for every row and group, in 32 bits
+    if (s->rows * ((long)s->width * s->page / 64 + 4) >= (1l << 31)) return LORY_ERR_SHAPE;
     if (groups > 0 && (long)(s->rows / groups) * (s->q_heads / s->kv_heads) >= (1l << 30)) return LORY_ERR_SHAPE;
     return LORY_OK;
 }

@@ -129,7 +129,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
         return paged::cache_row(a.div, at + (lane & (KEYS - 1)), page, a.pages, a.Hkv, kvh);
     };
     const int at0 = t0 * kTile<T> + wave * KEYS, page0 = page_of(at0), page1 = page_of(at0 + STEP);
-    w.load_q(0, a.q + b * a.q_row + (first + i) * a.q_head, a.D, c, i < nq);
+    W::load_q(w.q[0], a.q + b * a.q_row + (first + i) * a.q_head, a.D, c, i < nq);
     float m, l;
     auto walk = [&](auto split, int page, int next) {
         typename W::Keys x;
@@ -152,7 +152,7 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP, NW> &sh, int b, 
             const bool more = at + STEP < last;
 
             float p[1][NS], (&s)[NS] = p[0];
-            w.scores(0, x, s);
+            W::scores(w.q[0], x, s);
             if (more) W::load_k(x, a.k, max(row, 0), a.D, i, c);
 
             // rounded before the maximum is taken off: equal scores of any size stay equal (a fused product would not); to

@@ -35,7 +35,7 @@ struct Args {
     long out_row, out_head;   // bytes
     float *lse;
     int32_t *gstart, *rstart;   // workspace: units of one head before each group's prefix, each row; with the sum of all behind
-    float2 *part_o;             // pieces: [places][D / 2], a place a query
+    float *part_o;              // pieces: [places][D], a place a query
     float2 *part_ml;            // [places], maximum and sum
     long row_places, more_places;   // first place of the rows' pieces, and of pieces that do not begin an item
     int rows, groups, beams, Hq, Hkv, D, pages, page, width;
@@ -47,9 +47,6 @@ struct Args {
     float scale;
 };
 
-template <typename T> constexpr int kKeys = sizeof(T) == 2 ? 32 : 16;   // of a wavefront's step
-template <typename T> constexpr int kTile = kKeys<T> * kWaves;
-
 __device__ __forceinline__ int clamped(const Args &a, int n)
 {
     const int most = a.width * a.page;
@@ -60,17 +57,23 @@ __device__ __forceinline__ int shared_of(const Args &a, int g) { return clamped(
 // first token that a row reads by itself
 __device__ __forceinline__ int own_from(int len, int shared) { return len >= shared ? shared : 0; }
 
-template <typename T> __device__ __forceinline__ int units_of(int tokens) { return (tokens + kTile<T> - 1) / kTile<T>; }
+// Units of that many tokens, and what an item of them counts: as many, and kStart for finding its pages and joining its wavefronts.
+constexpr int kStart = 2;
+template <typename T> __device__ __forceinline__ int units_of(int tokens)
+{
+    return tokens > 0 ? (tokens + kTile<T> - 1) / kTile<T> + kStart : 0;
+}
 
-template <int DP> struct Shared {
-    float o[kWaves][16][DP + 4];   // a wavefront's output of one block, unnormalised
+template <int DP, int NQ> struct Shared {
+    u32x4 q[NQ * DP / 32 * 64];    // operands of the queries, DP / 32 pieces of 16 bytes a lane and block of bf16, twice that of fp32
+    alignas(16) float o[kWaves][16][DP + 4];   // a wavefront's output of one block, unnormalised
     float m[kWaves][16], l[kWaves][16];
 };
 
 // Tokens first .. last of the row whose table is `pages`, for key-value head kvh and nq queries; query(x): address of one, or
 // NULL: it takes no part.  The piece goes to the places from `place` on.
-template <typename T, int DP, bool PAD, bool STREAM, int NQ, typename Query>
-__device__ __forceinline__ void piece(const Args &a, Shared<DP> &sh, const int32_t *pages, int kvh, int first, int last, int nq,
+template <typename T, int DP, bool PAD, bool STREAM, int NQ, typename Lds, typename Query>
+__device__ __forceinline__ void piece(const Args &a, Lds &sh, const int32_t *pages, int kvh, int first, int last, int nq,
                                       long place, const Query &query)
 {
     using W = Wave<T, DP, PAD, NQ>;
@@ -86,11 +89,16 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP> &sh, const int32
         return paged::cache_row(a.div, at + (lane & (KEYS - 1)), page, a.pages, a.Hkv, kvh);
     };
     const int at0 = first + wave * KEYS, page0 = page_of(at0), page1 = page_of(at0 + STEP);
+    // the queries' operands lie in LDS: registers are what limits the wavefronts that run
+    constexpr int KS = W::KS;
+    if (wave < NQ) {
+        const char *p = wave * 16 + i < nq ? query(wave * 16 + i) : nullptr;
+        typename W::Query q;
+        W::load_q(q, p, a.D, c, p != nullptr);
 #pragma unroll
-    for (int b = 0; b < NQ; ++b) {
-        const char *p = b * 16 + i < nq ? query(b * 16 + i) : nullptr;
-        w.load_q(b, p, a.D, c, p != nullptr);
+        for (int s = 0; s < KS; ++s) sh.q[(wave * KS + s) * 64 + lane] = __builtin_bit_cast(u32x4, q[s]);
     }
+    __syncthreads();
     float m[NQ], l[NQ];
     auto walk = [&](auto split, int page, int next) {
         typename W::Keys x;
@@ -115,8 +123,14 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP> &sh, const int32
             const bool more = at + STEP < last;
 
             float s[NQ][NS];
+            asm volatile("" ::: "memory");   // the queries are read in every step: kept in registers they would cost others their place
 #pragma unroll
-            for (int b = 0; b < NQ; ++b) w.scores(b, x, s[b]);
+            for (int b = 0; b < NQ; ++b) {
+                typename W::Query q;
+#pragma unroll
+                for (int t = 0; t < KS; ++t) q[t] = __builtin_bit_cast(typename std::remove_reference<decltype(q[0])>::type, sh.q[(b * KS + t) * 64 + lane]);
+                W::scores(q, x, s[b]);
+            }
             if (more) W::load_k(x, a.k, max(row, 0), a.D, i, c);
             const bool full = valid == paged::all_keys(KEYS);
             if (!full) W::clear_v(x, valid, c);
@@ -161,7 +175,6 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP> &sh, const int32
         if (__builtin_expect(__any(odd), 0)) walk(std::true_type(), page_of(at0), page_of(at0 + STEP));
     }
 
-    const int pairs = a.D / 2;
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
         const int n = min(16, nq - 16 * b);
@@ -178,23 +191,31 @@ __device__ __forceinline__ void piece(const Args &a, Shared<DP> &sh, const int32
                 for (int r = 0; r < 4; ++r) sh.o[wave][i][W::dim(t, 4 * c + r)] = w.o[b][t][r];
         }
         __syncthreads();
-        for (int x = tid; x < n * pairs; x += kThreads) {
-            const int j = x / pairs, d = (x - j * pairs) * 2;
+        const int j = tid / 16;   // 16 threads a query, four dims at a time
+        if (j < n) {
             float M = sh.m[0][j];
 #pragma unroll
             for (int v = 1; v < kWaves; ++v) M = fmaxf(M, sh.m[v][j]);
             const float ref = M == -INFINITY ? 0.f : M;
-            float S = 0.f, O0 = 0.f, O1 = 0.f;
+            float S = 0.f, f[kWaves];
 #pragma unroll
             for (int v = 0; v < kWaves; ++v) {
-                const float f = exp_of(sh.m[v][j] - ref);
-                S = fmaf(f, sh.l[v][j], S);
-                O0 = fmaf(f, sh.o[v][j][d], O0);
-                O1 = fmaf(f, sh.o[v][j][d + 1], O1);
+                f[v] = exp_of(sh.m[v][j] - ref);
+                S = fmaf(f[v], sh.l[v][j], S);
             }
             const long to = place + 16 * b + j;
-            a.part_o[to * pairs + d / 2] = make_float2(O0, O1);
-            if (d == 0) a.part_ml[to] = make_float2(M, S);
+            float *out = a.part_o + to * a.D;
+            for (int d = tid % 16 * 4; d < a.D; d += 64) {
+                f32x4 O = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int v = 0; v < kWaves; ++v) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(&sh.o[v][j][d]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) O[e] = fmaf(f[v], x[e], O[e]);
+                }
+                *reinterpret_cast<f32x4 *>(out + d) = O;
+            }
+            if (tid % 16 == 0) a.part_ml[to] = make_float2(M, S);
         }
         __syncthreads();
     }
@@ -215,9 +236,16 @@ __device__ __forceinline__ Cut cut_of(const Args &a, long group_units, long row_
     return c;
 }
 
-template <typename T, int DP, bool PAD, bool STREAM, int NQ> __global__ __launch_bounds__(kThreads) void prefix_attn_kernel(Args a)
+// Workgroups of four wavefronts that the registers let a CU hold.
+constexpr int resident(int esize, int head_dim, int nq)
 {
-    __shared__ Shared<DP> sh;
+    return head_dim <= 64 ? (esize == 4 || nq == 1 ? 3 : 2) : head_dim <= 128 ? (nq <= 2 ? 2 : 1) : 1;
+}
+
+template <typename T, int DP, bool PAD, bool STREAM, int NQ>
+__global__ __launch_bounds__(kThreads, resident(sizeof(T), DP, NQ)) void prefix_attn_kernel(Args a)
+{
+    __shared__ Shared<DP, (sizeof(T) / 2) * NQ> sh;
     __shared__ int wsum[2][kWaves];
     __shared__ struct { int item, rest_units; long rest; } from[2];   // group or row of the range's first unit, and units of it before that
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -299,6 +327,7 @@ template <typename T, int DP, bool PAD, bool STREAM, int NQ> __global__ __launch
         int h = (int)paged::quotient64(from[0].rest, units), tile = (int)(from[0].rest - (long)h * units);
         while (u < uend) {
             const int shared = shared_of(a, g), stop = (int)(uend - u < units - tile ? tile + (uend - u) : units);
+            const int t0 = max(0, tile - kStart), t1 = stop - kStart;
             // a row that has all of the prefix: its table is read
             int has = INT32_MAX;
             for (int r = lane; r < a.beams; r += 64)
@@ -307,15 +336,15 @@ template <typename T, int DP, bool PAD, bool STREAM, int NQ> __global__ __launch
             for (int o = 1; o < 64; o <<= 1) has = min(has, __shfl_xor(has, o, 64));
             has = __builtin_amdgcn_readfirstlane(has);
             const int kvh = a.chunks == 1 ? h : h / a.chunks, q0 = (h - kvh * a.chunks) * 16 * NQ;
-            if (has != INT32_MAX) {
+            if (has != INT32_MAX && t0 < t1) {
                 auto query = [&](int x) -> const char * {
                     const int r = (q0 + x) / a.group, b = g * a.beams + r;
                     if (length_of(a, b) < shared) return nullptr;
                     return a.q + b * a.q_row + (kvh * a.group + (q0 + x) - r * a.group) * a.q_head;
                 };
-                piece<T, DP, PAD, false, NQ>(a, sh, a.table + ((long)g * a.beams + has) * a.table_row, kvh, tile * kTile<T>,
-                                              min(stop * kTile<T>, shared), min(16 * NQ, a.queries - q0),
-                                              tile == 0 ? ((long)g * gheads + h) * 16 * NQ : a.more_places + (long)w * 16 * NQ, query);
+                piece<T, DP, PAD, false, NQ>(a, sh, a.table + ((long)g * a.beams + has) * a.table_row, kvh, t0 * kTile<T>,
+                                              min(t1 * kTile<T>, shared), min(16 * NQ, a.queries - q0),
+                                              t0 == 0 ? ((long)g * gheads + h) * 16 * NQ : a.more_places + (long)w * 16 * NQ, query);
             }
             u += stop - tile;
             tile = 0;
@@ -330,13 +359,15 @@ template <typename T, int DP, bool PAD, bool STREAM, int NQ> __global__ __launch
         int h = (int)paged::quotient64(from[1].rest, units), tile = (int)(from[1].rest - (long)h * units);
         while (v < vend) {
             const int stop = (int)(vend - v < units - tile ? tile + (vend - v) : units);
+            const int t0 = max(0, tile - kStart), t1 = stop - kStart;
             const int len = length_of(a, b), start = own_from(len, shared_of(a, b / a.beams));
             const int kvh = a.tiles == 1 ? h : h / a.tiles, head = kvh * a.group + (h - kvh * a.tiles) * 16;
             const int nq = min(16, (kvh + 1) * a.group - head), most = min(16, a.group);
             auto query = [&](int x) -> const char * { return a.q + b * a.q_row + (head + x) * a.q_head; };
-            piece<T, DP, PAD, STREAM, 1>(a, sh, a.table + b * a.table_row, kvh, start + tile * kTile<T>,
-                                         min(start + stop * kTile<T>, len), nq,
-                                         tile == 0 ? a.row_places + ((long)b * rheads + h) * most : a.more_places + (long)w * 16 * NQ, query);
+            if (t0 < t1)
+                piece<T, DP, PAD, STREAM, 1>(a, sh, a.table + b * a.table_row, kvh, start + t0 * kTile<T>,
+                                         min(start + t1 * kTile<T>, len), nq,
+                                         t0 == 0 ? a.row_places + ((long)b * rheads + h) * most : a.more_places + (long)w * 16 * NQ, query);
             v += stop - tile;
             tile = 0;
             if (stop == units && ++h == rheads && v < vend) {
@@ -360,11 +391,11 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void prefix_att
     const Cut cut = cut_of(a, a.gstart[a.groups], a.rstart[a.rows]);
     for (int b = blockIdx.y; b < a.rows; b += gridDim.y) {
         const int g = b / a.beams, len = length_of(a, b), shared = shared_of(a, g);
-        const int gunits = len >= shared ? a.gstart[g + 1] - a.gstart[g] : 0, runits = a.rstart[b + 1] - a.rstart[b];
+        const int gspan = a.gstart[g + 1] - a.gstart[g], runits = a.rstart[b + 1] - a.rstart[b], gunits = len >= shared ? gspan : 0;
         int rw0 = 0, rparts = 0;
         if (runits > 0) {
             const long u = cut.prefix + (long)a.rstart[b] * rheads + (long)h * runits;
-            rw0 = paged::owner(u, cut.all, cut.ranges);
+            rw0 = paged::owner(u + kStart, cut.all, cut.ranges);
             rparts = paged::owner(u + runits - 1, cut.all, cut.ranges) - rw0 + 1;
         }
         const int quads = a.D / 4, all = nq * quads;
@@ -379,7 +410,7 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void prefix_att
             int gw0 = 0, gparts = 0;
             if (gunits > 0) {
                 const long u = (long)a.gstart[g] * gheads + (long)(kvh * a.chunks + c) * gunits;
-                gw0 = paged::owner(u * a.weight, cut.all, cut.ranges);
+                gw0 = paged::owner((u + kStart) * a.weight, cut.all, cut.ranges);
                 gparts = paged::owner((u + gunits - 1) * a.weight, cut.all, cut.ranges) - gw0 + 1;
             }
             const int parts = gparts + rparts;
@@ -409,7 +440,7 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void prefix_att
                     if (p0 + n * shares < parts) {
                         const long from = place_of(p0 + n * shares);
                         ml[n] = a.part_ml[from];
-                        o[n] = *reinterpret_cast<const f32x4 *>(a.part_o + from * 2 * quads + 2 * d);
+                        o[n] = *reinterpret_cast<const f32x4 *>(a.part_o + from * 4 * quads + 4 * d);
                     }
                 }
 #pragma unroll
@@ -441,16 +472,9 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void prefix_att
 int blocks(const lory_paged_shape &s, int groups)
 {
     const long n = groups > 0 ? (long)(s.rows / groups) * (s.q_heads / s.kv_heads) : 1;
-    int most = s.head_dim > 128 ? 1 : s.dtype == LORY_F32 ? 2 : 4;
+    int most = s.head_dim > 128 ? 1 : s.dtype == LORY_F32 || s.head_dim > 64 ? 2 : 4;
     while (most > 1 && n <= 8 * most) most /= 2;
     return most;
-}
-
-// Workgroups that run at a time.
-int ranges(const lory_paged_shape &s, int nq)
-{
-    const int wide = s.head_dim <= 64 ? 0 : s.head_dim <= 128 ? 1 : 2;
-    return kCUs * (nq == 4 ? 1 : nq == 2 ? (wide == 0 ? 2 : 1) : wide == 0 ? 3 : wide == 1 ? 2 : 1);
 }
 
 struct Sizes {
@@ -461,7 +485,7 @@ struct Sizes {
     {
         const int group = s.q_heads / s.kv_heads;
         nq = blocks(s, groups);
-        ranges = lory::ranges(s, nq);
+        ranges = kCUs * resident(s.dtype == LORY_F32 ? 4 : 2, s.head_dim, nq);
         const long n = groups > 0 ? (long)(s.rows / groups) * group : 0;
         chunks = (int)((n + 16 * nq - 1) / (16 * nq));
         tiles = (group + 15) / 16;
@@ -488,7 +512,7 @@ template <typename T, int DP, bool PAD, int NQ> void launch4(const Args &a, bool
 
 template <typename T, int DP, bool PAD> void launch3(const Args &a, int nq, bool stream, hipStream_t st)
 {
-    constexpr int most = DP > 128 ? 1 : sizeof(T) == 4 ? 2 : 4;
+    constexpr int most = DP > 128 ? 1 : sizeof(T) == 4 || DP > 64 ? 2 : 4;
     if (nq == 1) return launch4<T, DP, PAD, 1>(a, stream, st);
     if constexpr (most >= 2) {
         if (nq == 2) return launch4<T, DP, PAD, 2>(a, stream, st);
@@ -540,7 +564,7 @@ int prefix_attn_launch(const lory_paged_shape &s, int groups, const lory_heads &
     a.lse = lse;
     a.gstart = (int32_t *)ws;
     a.rstart = (int32_t *)((char *)ws + z.gstart);
-    a.part_o = (float2 *)((char *)ws + z.gstart + z.rstart);
+    a.part_o = (float *)((char *)ws + z.gstart + z.rstart);
     a.part_ml = (float2 *)((char *)ws + z.gstart + z.rstart + z.o);
     a.row_places = z.row_places;
     a.more_places = z.more_places;
