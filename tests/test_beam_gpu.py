@@ -568,3 +568,189 @@ def test_prefix_attention_cache_above_32_bits():
     lens, shared = i32([7 * page, 6 * page + 5, 5 * page]), i32([6 * page])
     case = (q, k, v, table, lens)
     check_attention("far pages", *prefixed(case, shared), *case)
+
+
+# ---------------------------------------------------------------- all together
+
+class Search:
+    """A beam search over a paged cache: plan, store, attention, selection, fork, copies; two sets of tables that change places."""
+
+    def __init__(self, B=3, K=4, Hq=8, Hkv=2, D=64, page=8, prompt=(5, 40, 16), steps=24, V=500, layers=2):
+        self.B, self.K, self.Hkv, self.D, self.page, self.V = B, K, Hkv, D, page, V
+        R, W = B * K, -(-(max(prompt) + steps + 4) // page)
+        self.pages = F = B * (-(-max(prompt) // page)) + R * (-(-steps // page) + 2) + 7
+        z = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+        self.lens, self.table, self.count = [z(R), z(R)], [z(R, W) - 1, z(R, W) - 1], [z(1), z(1), z(1)]
+        self.free = torch.arange(F, dtype=torch.int32, device="cuda")
+        self.count[0].fill_(F)
+        self.add, self.cu, self.status, self.fork_status = z(R), z(R + 1), z(1), z(1)
+        self.positions, self.slots = z(R), torch.zeros(R, dtype=torch.int64, device="cuda")
+        self.planned, self.copies, self.shared = z(R), z(3, R), z(B)
+        self.cache = [torch.zeros(layers, F, Hkv, page, D, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+        self.qkv = torch.zeros(R, (Hq + 2 * Hkv) * D, device="cuda", dtype=torch.bfloat16)
+        self.q, self.kx, self.vx = (x.unflatten(1, (-1, D)) for x in self.qkv.split([Hq * D, Hkv * D, Hkv * D], 1))
+        self.y, self.out = (torch.empty(R, Hq, D, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+        self.freq = torch.from_numpy(10000.0 ** (-2.0 * np.arange(D // 2) / D)).cuda()
+        self.logits, self.score = torch.zeros(R, V, device="cuda", dtype=torch.bfloat16), torch.zeros(B, K, device="cuda")
+        self.score_new, self.token, self.parent = torch.zeros(B, K, device="cuda"), z(B, K), z(B, K)
+        self.ws = [lb.alloc_beam_select_workspace(self.logits, self.score, K), lb.alloc_kv_fork_workspace(z(R), self.table[0], F),
+                   lb.alloc_prefix_attn_workspace(self.q, self.cache[0][0], self.table[0], self.shared)]
+        self.lse = torch.zeros(R, Hq, device="cuda")
+
+    def start(self, prompt, g):
+        """Prompts of one row a request, stored into both layers, and forked into beams."""
+        B, K = self.B, self.K
+        n = sum(prompt)
+        i = lambda a: i32(a)
+        lens, table = i([0] * B), self.table[1][:B]
+        pos, slots = i([0] * n), torch.zeros(n, dtype=torch.int64, device="cuda")
+        new, cu = i([0] * B), i([0] * (B + 1))
+        lb.lory_kv_plan(lens, i(prompt), table, self.free, self.count[0], self.page, new, cu, pos, slots, self.count[1], self.status)
+        x = rnd(g, n, self.Hkv, self.D, dtype=torch.bfloat16)
+        q = rnd(g, n, self.q.shape[1], self.D, dtype=torch.bfloat16)
+        for layer in range(self.cache[0].shape[0]):
+            lb.lory_qk_rope_cache(q, x, x, pos, self.freq, self.cache[0][layer], self.cache[1][layer], slots)
+        lb.lory_kv_fork(new, i(np.repeat(np.arange(B), K)), table, self.free, self.count[1], self.page, self.pages, self.lens[0],
+                        self.table[0], self.count[0], self.copies, self.fork_status)
+        lb.lory_kv_copy(*self.cache, self.copies)
+        self.shared.copy_(i(prompt))
+        self.score[:, 1:] = NONE
+
+    def step(self, a, b):
+        """From set a to set b."""
+        self.attend(a)
+        self.choose(a, b)
+
+    def attend(self, a):
+        lb.lory_kv_plan(self.lens[a], self.add, self.table[a], self.free, self.count[0], self.page, self.planned, self.cu, self.positions,
+                        self.slots, self.count[1], self.status)
+        for layer in range(self.cache[0].shape[0]):
+            lb.lory_qk_rope_cache(self.q, self.kx, self.vx, self.positions, self.freq, self.cache[0][layer], self.cache[1][layer],
+                                  self.slots, q_out=self.y)
+        lb.lory_prefix_attn(self.y, self.cache[0][1], self.cache[1][1], self.table[a], self.planned, self.shared, out=self.out, lse=self.lse,
+                            workspace=self.ws[2])
+
+    def choose(self, a, b):
+        self.logits += self.out.flatten(1).float().sum(1, keepdim=True).bfloat16()
+        lb.lory_beam_select(self.logits, self.score, self.K, score_out=self.score_new, token=self.token, parent=self.parent,
+                            workspace=self.ws[0])
+        lb.lory_kv_fork(self.planned, self.parent.view(-1), self.table[a], self.free, self.count[1], self.page, self.pages, self.lens[b],
+                        self.table[b], self.count[0], self.copies, self.fork_status, workspace=self.ws[1])
+        lb.lory_kv_copy(*self.cache, self.copies)
+        self.score.copy_(self.score_new)
+
+    def rows(self, a):
+        """Keys and values of every row of set a, in both layers."""
+        out = []
+        for b, n in enumerate(self.lens[a].tolist()):
+            pages = self.table[a][b].long()[:-(-n // self.page)]
+            out.append([x[:, pages].transpose(1, 2).flatten(2, 3)[:, :, :n] for x in self.cache] if n else [])
+        return out
+
+
+def feed(s, g):
+    """What a model would compute: new queries, keys and values, and logits."""
+    qkv, logits = rnd(g, *s.qkv.shape, dtype=torch.bfloat16), (3 * rnd(g, *s.logits.shape)).bfloat16()
+    return qkv, logits
+
+
+def test_beam_search_over_the_cache():
+    """A search with ended beams against dense copies of every row's keys and values; pages are neither lost nor shared wrongly."""
+    prompt, g = (5, 40, 16), gen(0)
+    s = Search(prompt=prompt)
+    s.start(prompt, g)
+    R, K = s.B * s.K, s.K
+    s.add.fill_(1)
+    dense = s.rows(0)
+    assert s.lens[0].tolist() == np.repeat(prompt, K).tolist() and s.fork_status.item() == 0
+    for b in range(R):     # all beams of a request have its prompt
+        assert all(torch.equal(x, y) for x, y in zip(dense[b], dense[b // K * K]))
+    for step in range(24):
+        a, b = step % 2, 1 - step % 2
+        qkv, logits = feed(s, g)
+        s.qkv.copy_(qkv)
+        s.logits.copy_(logits)
+        if step == 9:
+            s.score[1, 1:] = NONE                      # all beams of request 1 but one have ended
+        if step == 15:
+            s.logits[:, 2:] = NONE                     # two tokens may follow: fewer candidates than beams for some
+        score = s.score.clone()
+        s.attend(a)
+        if step % 8 == 0:   # before pages change hands
+            check_attention(f"step {step}", s.out, s.lse, s.y, s.cache[0][1], s.cache[1][1], s.table[a], s.planned)
+        s.choose(a, b)
+        assert s.status.item() == 0 and s.fork_status.item() == 0
+        check_select(f"step {step}", s.logits, score, K, (s.score_new, s.token, s.parent))
+        k_new, v_new = lb.lory_qk_rope(s.q, s.kx, s.positions, s.freq)[1], s.vx
+        grown = [[torch.cat([x, n[r][None, :, None].expand(2, -1, -1, -1)], 2) for x, n in zip(dense[r], (k_new, v_new))] if dense[r] else []
+                 for r in range(R)]
+        dense = [grown[p] if p >= 0 else [] for p in s.parent.view(-1).tolist()]
+        for r, (x, y) in enumerate(zip(s.rows(b), dense)):
+            assert len(x) == len(y) and all(torch.equal(m, n) for m, n in zip(x, y)), (step, r)
+        # rows without a token add none, and theirs are not a plan's any more
+        s.add.copy_((s.lens[b] > 0).int())
+        if (s.lens[b] == 0).any():
+            break
+        used = {p for r, n in enumerate(s.lens[b].tolist()) for p in s.table[b][r, :-(-n // s.page)].tolist()}
+        free = s.free[:s.count[0].item()].tolist()
+        assert len(set(free)) == len(free) and not used & set(free) and len(used) + len(free) == s.pages
+        last = [s.table[b][r, (n - 1) // s.page].item() for r, n in enumerate(s.lens[b].tolist()) if n % s.page]
+        assert len(set(last)) == len(last)             # a page that is written next belongs to one row
+    assert step >= 15
+
+
+def test_search_on_another_stream_and_in_a_graph():
+    """Two steps, there and back between the sets, run eagerly, on a side stream and from a graph; every replay against the eager run."""
+    prompt, g = (5, 40, 16), gen(1)
+    searches = [Search(prompt=prompt, steps=40) for _ in range(3)]
+    for s in searches:
+        s.start(prompt, gen(2))
+        s.add.fill_(1)
+    eager, side, captured = searches
+    warm = Search(prompt=prompt)
+    warm.start(prompt, gen(2))
+    warm.step(0, 1)
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    keep = [x.clone() for x in (captured.free, captured.score)]
+    with torch.cuda.graph(graph):
+        captured.step(0, 1)
+        captured.step(1, 0)
+    assert torch.equal(keep[0], captured.free) and torch.equal(keep[1], captured.score)
+    for i in range(15):
+        qkv, logits = feed(eager, g)
+        for s in searches:
+            s.qkv.copy_(qkv)
+            s.logits.copy_(logits)
+        eager.step(0, 1)
+        eager.step(1, 0)
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):
+            side.step(0, 1)
+            side.step(1, 0)
+        torch.cuda.current_stream().wait_stream(stream)
+        graph.replay()
+        junk = torch.randn(1000, 1000, device="cuda")
+        (junk @ junk).sum().item()
+        for s in (side, captured):
+            for n in ("free", "status", "fork_status", "positions", "slots", "planned", "copies", "y", "out", "lse", "logits", "score", "token",
+                      "parent"):
+                assert torch.equal(getattr(s, n), getattr(eager, n)), (i, n)
+            for n in ("lens", "table", "count", "cache"):
+                assert all(torch.equal(x, y) for x, y in zip(getattr(s, n), getattr(eager, n))), (i, n)
+        assert eager.status.item() == 0 and eager.fork_status.item() == 0
+    assert eager.lens[0].tolist() == (np.repeat(prompt, 4) + 30).tolist()
+
+
+def test_event_timing_knows_the_operators_of_a_search():
+    s = Search()
+    s.start((5, 40, 16), gen(0))
+    lb.lory_profile_read()
+    lb.lory_profile_enable(True)
+    try:
+        s.step(0, 1)
+        got = {r["name"]: r for r in lb.lory_profile_read()}
+    finally:
+        lb.lory_profile_enable(False)
+    assert set(got) == {"qk_rope", "kv_plan", "beam_select", "kv_fork", "kv_copy", "prefix_attn"}
+    assert all(got[n]["launches"] == 1 and got[n]["ms"] > 0 for n in ("beam_select", "kv_fork", "kv_copy", "prefix_attn"))
+    assert got["beam_select"]["bytes"] == 12 * 500 * 2
