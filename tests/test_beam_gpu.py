@@ -754,3 +754,40 @@ def test_event_timing_knows_the_operators_of_a_search():
     assert set(got) == {"qk_rope", "kv_plan", "beam_select", "kv_fork", "kv_copy", "prefix_attn"}
     assert all(got[n]["launches"] == 1 and got[n]["ms"] > 0 for n in ("beam_select", "kv_fork", "kv_copy", "prefix_attn"))
     assert got["beam_select"]["bytes"] == 12 * 500 * 2
+
+
+@pytest.mark.parametrize("dtype", [torch.float32])
+def test_beam_example(dtype):
+    """The example's search: its beams' scores are those of their tokens, run one by one as rows of their own."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "generate_beams.py")
+    spec = importlib.util.spec_from_file_location("generate_beams", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    block = m.Block(d=64, heads=4, kv_heads=2, head_dim=16, d_ff=128, experts=4, dtype=dtype)
+    g = gen(4)
+    B, L, K, V, steps, page = 3, 21, 4, 90, 9, 8
+    head = (rnd(g, block.d, V) * block.d ** -0.5).to(dtype)
+    prompts, lens = rnd(g, B, L, block.d).to(dtype), i32([5, 21, 16])
+    score, tokens, status, count = m.search(block, prompts, lens, head, K, steps, page)
+    assert [s.item() for s in status] == [0, 0] and tokens.shape == (B, K, steps) and (tokens >= 0).all()
+    assert len({tuple(t) for t in tokens[1].tolist()}) == K and (score[:, 1:] <= score[:, :-1]).all()
+    # pages in use: of the prompts' whole pages one set a request, and at most ceil(steps / page) + 1 a beam
+    pages = B * -(-L // page) + B * K * (-(-steps // page) + 2)
+    assert count.item() >= pages - sum(-(-n // page) for n in lens.tolist()) - B * K * (-(-steps // page) + 1)
+    for k in range(K):      # beam k of every request as a batch of single rows
+        r = m.Requests(block, B, 60, page, L + steps)
+        h, merged = m.prefill(block, r, prompts, lens)
+        h = m.next_input(h[torch.arange(B, device="cuda"), lens.long() - 1])
+        total = torch.zeros(B, dtype=torch.float64, device="cuda")
+        one = m.Beams(r, lens, B, 1, 60)
+        one.shared.zero_()
+        for t in range(steps):
+            token = tokens[:, k, t].long()
+            total += torch.log_softmax((h @ head).double(), 1).gather(1, token[:, None])[:, 0]
+            if t + 1 < steps:
+                h = m.next_input(m.decode(block, one, m.next_input(head.T[token].contiguous()), merged))
+        # fp32 all along; the merged FFN adds in another order for several tokens of a sequence.  A step's logits are sums of
+        # 64 products of normalised states, off by at most a few hundred roundings of fp32 after the block: 9 steps of 1e-4
+        assert (score[:, k].double() - total).abs().max().item() < 9e-4, k
