@@ -7,7 +7,11 @@
 //
 // Small tables are one workgroup's, with the sets as bits in LDS.  Larger ones take three launches: the first children of the old rows, and
 // the sets cleared; the marks and the new tables; the sums, by one workgroup.  There the sets are bytes, set by plain stores: bits
-// need atomic operations that all XCDs see, 41 us for 512 rows of 95 pages where the bytes take a tenth.
+// need atomic operations that all XCDs see, 41 us for 512 rows of 95 pages where the bytes take 4.2.
+// Measured: 16 rows of up to 94 pages in one launch 5.3 us (three took 9.7 and two more starts); 512 rows of up to 260 pages 2.1 + 4.2 +
+// 5.6, 240 rows of up to 1600 2.0 + 5.0 + 6.1; the last launch is a chain of reads and two sums over its threads.
+//
+// lory_kv_copy is bound by HBM: 3001 pages of 128 KB 158.6 us, 4.96 TB/s read and written together, a large copy's rate.
 #include "lory_internal.h"
 
 namespace lory {

@@ -11,6 +11,13 @@
 // workgroup each; every range leaves the maximum, sum and unnormalised output of each item that it touches in the workspace, and a
 // second launch joins an output's pieces in order: those of its group's prefix and those of its row.
 //
+// Measured (us, both launches): 24 groups of 8 rows, prefixes of 300 to 6000 tokens, 16 heads of 128 on 4: 39.6 + 7.5; 96 rows, 16000
+// tokens in common, 32 heads on 8: 117.7 + 7.4; rows of one token of their own beside it 90 + 7.  Queries in registers instead of LDS, one workgroup a
+// CU: 50 and 161.  Blocks: of heads of 128 four to a wavefront (one workgroup a CU) 135 where two take 115; of heads of 64 four 80, two 89.
+// What an item counts beside its units: 1 150, 2 118, 4 130; the last tokens of every row left to the second launch instead: 31 + 22, 123 + 60.
+// Bound now: with few queries by the chain of a unit (page, keys, values: 2 us a step on four wavefronts) and of a piece's start and
+// end, 1.5 us; with hundreds by the steps' own instructions and the re-reads of the prefix, 489 MB where 361 are needed.
+//
 // A row is one of its group's where it has at least the group's shared tokens; a shorter one reads all its tokens by itself.
 #include "attn_wave.h"
 #include "lory_internal.h"
@@ -468,7 +475,8 @@ template <typename T> __global__ __launch_bounds__(kJoinThreads) void prefix_att
     }
 }
 
-// Blocks of 16 queries that a wavefront holds: as many as the rows of a group have, and the registers.
+// Blocks of 16 queries that a wavefront holds: as many as the rows of a group have, and as leave room for two workgroups on a CU
+// (measured on both sides, above).
 int blocks(const lory_paged_shape &s, int groups)
 {
     const long n = groups > 0 ? (long)(s.rows / groups) * (s.q_heads / s.kv_heads) : 1;
@@ -586,6 +594,7 @@ int prefix_attn_launch(const lory_paged_shape &s, int groups, const lory_heads &
     a.div = paged::divider(s.page);
     a.scale = s.scale;
     prof::Range r(st, prof::kPrefixAttn, 0.0, 0.0);   // the lengths are on the device
+    // rows' own values of large caches past them, from where paged_attn.hip measured it; a prefix may be read by several workgroups
     const bool stream = 2 * (long)s.pages * s.kv_heads * s.page * s.head_dim * esize > (64l << 20);
     if (s.dtype == LORY_F32)
         launch1<float>(a, z.nq, stream, st);
