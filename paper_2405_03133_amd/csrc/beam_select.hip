@@ -520,7 +520,7 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void beam_join_kern
     }
 }
 
-// Chunks of a row, and 16-byte vectors of a chunk: as many workgroups as run at a time (eight a CU) where the rows alone are fewer,
+// Chunks of a row, and 16-byte vectors of a chunk: as many workgroups as run at a time (four a CU) where the rows alone are fewer,
 // of one vector a thread at least.
 // Chunks of a row, and 16-byte vectors of a chunk: as many workgroups as run at a time (two a CU) where the rows alone are fewer,
 // chunks of eight thousand logits at least, and of what a workgroup's registers hold at most.
