@@ -20,7 +20,9 @@ namespace {
 
 constexpr int kThreads = 256, kLast = 1024;
 constexpr int kSmallRows = 2048, kSmallPages = 1 << 17;      // whose sets and first children LDS holds
-constexpr int kSmallEntries = 16384;                         // of both tables
+// Entries of both tables up to which one workgroup is faster, us called eagerly, one launch / three: 1024 5.5 / 10.6, 4416 7.4 / 10.2,
+// 8832 9.7 / 10.2, 17664 15.0 / 10.6, 33792 23.7 / 12.5.
+constexpr int kSmallEntries = 9000;
 constexpr int kFirstRows = 8192;                             // old rows of a workgroup that finds first children
 constexpr int kLocalWords = 8192;                            // of 32 pages, that the last launch packs by itself
 
