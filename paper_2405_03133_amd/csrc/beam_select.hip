@@ -220,17 +220,21 @@ template <typename T> __global__ __launch_bounds__(kThreads, kResident / 256) vo
             }
         }
     };
+    // Two questions to a vector, asked as one: does it reach the bound, and has its wavefront's reference to be raised?  The second does not
+    // follow from the first: the bound is the workgroup's, the reference the wavefront's own, which may have seen nothing but barred tokens.
+    float gate = fminf(least, ref.ref + 64.f);
     double sum = 0.0;
     auto take = [&](const gemm::u32x4 (&x)[kHead], int v) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < kHead; ++i) {
             const float mx = max_of<T>(x[i], -INFINITY);
-            if (__any(mx >= least && mx > -INFINITY)) {
+            if (__any(mx >= gate && mx > -INFINITY)) {
                 if (__any(mx > ref.ref + 64.f)) {   // a wavefront's sum stays far inside fp32
                     const double old = ref.top();
                     const bool none = ref.ref == -INFINITY;
                     ref.set(wave_max(mx));
+                    gate = fminf(least, ref.ref + 64.f);
                     sum = none ? 0.0 : (sum + s) * exp(old - ref.top());
                     s = 0.f;
                 }

@@ -1,0 +1,84 @@
+"""Selection over rows that a workgroup streams in several whole steps: barred tokens, jumps and orders that its reference of the
+exponentials, its bound and its lists of candidates have to follow.
+
+Bounds are those of check_select in test_beam_gpu.py.  They hold here too: an exponential's argument is taken from a reference that is at most
+24 below the logits that count (64 at most by the kernel's rule), so its rounding is 22 x 2^-24 at most beside the 34 of a group's sum and the exponential."""
+import pytest
+import torch
+
+from test_attn_gpu import T, gen, rnd
+from test_beam_gpu import NONE, check_select, logits_of
+
+pytestmark = pytest.mark.gpu
+
+PER = {"bf16": 8, "f32": 4}                       # logits of a 16-byte vector
+CHUNKS = 16                                       # of a row where rows are few
+VECTORS = 4096                                    # of a chunk in these tests: four whole steps of 1024, and nothing behind them
+LOW = {"far": -1e4, "billion": -1e9, "lowest": None, "none": NONE}
+
+
+def low(name, dtype):
+    return torch.finfo(T[dtype]).min if LOW[name] is None else LOW[name]
+
+
+def long_rows(g, rows, dtype, sigma=2.0):
+    return logits_of(g, rows, CHUNKS * VECTORS * PER[dtype], dtype, sigma)
+
+
+def by_vector(x, dtype):
+    """[rows, chunks, vectors of a chunk, logits of a vector], the same memory."""
+    return x.view(x.shape[0], CHUNKS, VECTORS, PER[dtype])
+
+
+def of_wavefront(w):
+    """Vectors of a chunk that wavefront w of a workgroup reads."""
+    return (torch.arange(VECTORS, device="cuda") % 256) // 64 == w
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("barred", list(LOW))
+@pytest.mark.parametrize("shift", [0.0, -200.0, 100.0])
+def test_select_where_a_wavefront_starts_barred(barred, shift, dtype):
+    """The first step of one wavefront, of two, and of all but one has only barred tokens; what comes later is ordinary, and most
+    of it no candidate."""
+    g = gen(7)
+    R, K, k = 3, 4, 6
+    x = by_vector(long_rows(g, R * K, dtype), dtype)
+    x += shift
+    first = torch.arange(VECTORS, device="cuda") < 1024
+    for r in range(R * K):
+        waves = [[r % 4], [r % 4, (r + 1) % 4], [w for w in range(4) if w != r % 4]][r // 4]
+        for w in waves:
+            x[r, :, first & of_wavefront(w)] = low(barred, dtype)
+    # and the best tokens all in the first step of the others: a bound that the wavefront's own logits stay below
+    x[:, :, 1024:] = torch.minimum(x[:, :, 1024:], torch.tensor(shift + 4.0, device="cuda", dtype=T[dtype]))
+    check_select(f"{barred} {shift}", x.view(R * K, -1), -torch.rand(R, K, generator=g, device="cuda"), k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("barred", list(LOW))
+@pytest.mark.parametrize("R,K,V,k", [(130, 4, 32000, 4), (18, 8, 128000, 8)])
+def test_select_where_few_tokens_are_allowed(R, K, V, k, barred, dtype):
+    """A constraint: twenty tokens anywhere, or two runs of them, of every row."""
+    g = gen(V + k)
+    full = logits_of(g, R * K, V, dtype)
+    allowed = torch.zeros(R * K, V, dtype=torch.bool, device="cuda")
+    allowed.scatter_(1, torch.randint(0, V, (R * K, 20), generator=g, device="cuda"), True)
+    allowed[::3, 30200:31200] = True
+    allowed[::3, :1000] = True
+    x = torch.where(allowed, full, torch.tensor(low(barred, dtype), device="cuda", dtype=T[dtype]))
+    check_select(f"few allowed, {barred}", x, -torch.rand(R, K, generator=g, device="cuda"), k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_select_after_a_low_prefix(dtype):
+    """Logits that jump by more than fp32's exponentials hold, once and again, at places that differ from row to row."""
+    g = gen(11)
+    R, K = 2, 4
+    x = long_rows(g, R * K, dtype)
+    n = x.shape[1]
+    at = torch.arange(n, device="cuda") % (n // CHUNKS)
+    for r in range(R * K):
+        x[r] -= 150.0 * ((at < 9000 + 1000 * r).float() + (at < 5000 + 500 * r).float()).to(T[dtype])
+    check_select("two jumps", x, torch.zeros(R, K, device="cuda"), 8)
+    check_select("two falls", x.flip(1).contiguous(), torch.zeros(R, K, device="cuda"), 8)
