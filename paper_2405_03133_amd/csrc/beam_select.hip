@@ -232,10 +232,10 @@ template <typename T> __global__ __launch_bounds__(kThreads, kResident / 256) vo
             if (__any(mx >= gate && mx > -INFINITY)) {
                 if (__any(mx > ref.ref + 64.f)) {   // a wavefront's sum stays far inside fp32
                     const double old = ref.top();
-                    const bool none = ref.ref == -INFINITY;
+                    const bool none = ref.ref == -INFINITY;   // so far 0, or NaN where a logit was that: it stays
                     ref.set(wave_max(mx));
                     gate = fminf(least, ref.ref + 64.f);
-                    sum = none ? 0.0 : (sum + s) * exp(old - ref.top());
+                    sum = none ? sum + s : (sum + s) * exp(old - ref.top());
                     s = 0.f;
                 }
                 note(mx, x[i], v + i * kThreads);

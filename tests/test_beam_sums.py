@@ -6,8 +6,8 @@ Bounds are those of check_select in test_beam_gpu.py.  They hold here too: an ex
 import pytest
 import torch
 
-from test_attn_gpu import T, gen, rnd
-from test_beam_gpu import NONE, check_select, logits_of
+from test_attn_gpu import T, gen
+from test_beam_gpu import NONE, check_select, logits_of, select
 
 pytestmark = pytest.mark.gpu
 
@@ -82,3 +82,25 @@ def test_select_after_a_low_prefix(dtype):
         x[r] -= 150.0 * ((at < 9000 + 1000 * r).float() + (at < 5000 + 500 * r).float()).to(T[dtype])
     check_select("two jumps", x, torch.zeros(R, K, device="cuda"), 8)
     check_select("two falls", x.flip(1).contiguous(), torch.zeros(R, K, device="cuda"), 8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_select_nan_among_barred_tokens(dtype):
+    """A wavefront meets a NaN before its first number: the beam has no candidates, and the others keep theirs."""
+    g = gen(13)
+    R, K = 3, 4
+    x = by_vector(long_rows(g, R * K, dtype), dtype)
+    at = torch.arange(VECTORS, device="cuda")
+    odd = []
+    for r in range(R * K):
+        w = r % 4
+        x[r, 5, (at < 2048) & of_wavefront(w)] = NONE
+        if r % K != r // K:
+            continue
+        x[r, 5, 1024 + 64 * w + 11, PER[dtype] - 1] = float("nan")
+        odd.append(r)
+    x = x.view(R * K, -1)
+    score = -torch.rand(R, K, generator=g, device="cuda")
+    check_select("NaN among -inf", x, score, 8)
+    _, _, parent = select(x, score, 8)
+    assert not torch.isin(parent, torch.tensor(odd, device="cuda", dtype=torch.int32)).any()
