@@ -6,6 +6,7 @@ Bounds are those of check_select in test_beam_gpu.py.  They hold here too: an ex
 import pytest
 import torch
 
+from paper_2405_03133_amd import binding as lb
 from test_attn_gpu import T, gen
 from test_beam_gpu import NONE, check_select, logits_of, select
 
@@ -104,3 +105,31 @@ def test_select_nan_among_barred_tokens(dtype):
     check_select("NaN among -inf", x, score, 8)
     _, _, parent = select(x, score, 8)
     assert not torch.isin(parent, torch.tensor(odd, device="cuda", dtype=torch.int32)).any()
+
+
+def steps_per_vocab(dtype, order, V, k):
+    """Seconds of a call on a row whose logits come in that order, the best of a few."""
+    x = torch.linspace(-10.0, 10.0, V, device="cuda", dtype=torch.float64).to(T[dtype])[None]
+    x = {"up": x, "down": x.flip(1)}[order].contiguous()
+    score, best = torch.zeros(1, 1, device="cuda"), []
+    ws = lb.alloc_beam_select_workspace(x, score, k)
+    for _ in range(4):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        lb.lory_beam_select(x, score, k, workspace=ws)
+        b.record()
+        torch.cuda.synchronize()
+        best.append(a.elapsed_time(b))
+    check_select(f"{order} {V}", x, score, k)
+    return min(best)
+
+
+@pytest.mark.parametrize("order", ["up", "down"])
+@pytest.mark.parametrize("dtype,k", [("bf16", 4), ("f32", 1), ("f32", 64)])
+def test_select_of_sorted_logits(order, dtype, k):
+    """Every vector beats all before it, and so does every one of a chunk: the time grows as the row does, not as its square
+    (eight times the row: 64)."""
+    V = 1 << 18 if dtype == "f32" else 1 << 19
+    short, long = steps_per_vocab(dtype, order, V, k), steps_per_vocab(dtype, order, 8 * V, k)
+    print(f"[beam] {order} {dtype} k {k}: {short * 1e3:.0f} us, {long * 1e3:.0f} us", flush=True)
+    assert long <= 16 * short
