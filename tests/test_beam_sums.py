@@ -133,3 +133,36 @@ def test_select_of_sorted_logits(order, dtype, k):
     short, long = steps_per_vocab(dtype, order, V, k), steps_per_vocab(dtype, order, 8 * V, k)
     print(f"[beam] {order} {dtype} k {k}: {short * 1e3:.0f} us, {long * 1e3:.0f} us", flush=True)
     assert long <= 16 * short
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("k", [1, 7, 64])
+def test_select_of_equal_logits_in_long_rows(k, dtype):
+    """Every vector of every step equals the bound: the lowest tokens of the first beam; and two values, the larger one rare."""
+    R, K = 2, 2
+    x = torch.zeros(R * K, CHUNKS * VECTORS * PER[dtype], device="cuda", dtype=T[dtype])
+    score = torch.zeros(R, K, device="cuda")
+    _, token, parent = select(x, score, k)
+    assert (token == torch.arange(k, device="cuda")).all() and (parent == torch.tensor([[0], [K]], device="cuda")).all()
+    g = gen(k)
+    x[torch.rand(x.shape, generator=g, device="cuda") < 1e-5] = 0.5
+    check_select("rare", x, score, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [8, 16, 64])
+def test_select_of_more_equal_candidates_than_a_list_holds(K, dtype):
+    """k equal candidates of every chunk of every beam, 8192 and more of a request: the first beam's, whatever list they came in;
+    with different scores the best beam's."""
+    k, V = 64, 40000
+    x = torch.zeros(2 * K, V, device="cuda", dtype=T[dtype])
+    score = torch.zeros(2, K, device="cuda")
+    score[1, K - 2:] = 1.0
+    _, token, parent = select(x, score, k)
+    assert (token == torch.arange(k, device="cuda")).all() and (parent[0] == 0).all() and (parent[1] == 2 * K - 2).all()
+    # ten better tokens of every beam, at other places in each: the sums are those of the same terms, rounded in another order, so
+    # which beam comes first is the sums' affair
+    n = torch.arange(10, device="cuda")
+    for b in range(2 * K):
+        x[b, (n * 3989 + 17 * b) % V] = 1.0
+    check_select("few better ones", x, score, k)
