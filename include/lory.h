@@ -504,8 +504,8 @@ int lory_paged_attn(const lory_paged_shape *shape, const lory_heads *q, const vo
  *      the row request * beams + b.  A z of -inf or NaN is no candidate, so a logit of
  *      -inf bars its token, and a beam with a logit of NaN or +inf has none.  Where a request has
  *      fewer than k candidates the last places have score -inf, token -1, parent -1.
- * The order is that of z in fp64 (sums over a row: fp32 in groups of 32 logits,
- * fp64 over them); score_out is rounded once.
+ * The order is that of z in fp64 (sums over a row: fp32 in groups of 32 logits of
+ * bf16, 16 of fp32, fp64 over them); score_out is rounded once.
  * 1 <= beams <= 64, 1 <= k <= 64, 1 <= vocab <= 2^24, requests * beams <= 2^20.
  * No output may overlap another array.
  * workspace: lory_beam_select_workspace_bytes(shape); contents undefined before

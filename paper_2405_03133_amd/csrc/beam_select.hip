@@ -5,16 +5,17 @@
 // Bound by the bytes of the logits, read once; four operations each, one of them an exponential (a quarter of the others' rate).  A request's
 // k best are among the k best of each of its beams, and within a beam they are those of the logits themselves, whatever the sum is: so
 // a workgroup streams a chunk of one beam's logits, adds its exponentials and keeps its k largest logits, and a second launch forms
-// the sums, ranks what the chunks of a request left, and writes.  Sums of a lane (32 terms) are fp32, all others and the ranking
-// fp64: candidates of different beams may be as near each other as the sums are accurate.
+// the sums, ranks what the chunks of a request left, and writes.  Sums of a lane (32 terms of bf16, 16 of fp32) are fp32, all others and the
+// ranking fp64: candidates of different beams may be as near each other as the sums are accurate.
 //
 // The k largest of a chunk: of its first part every two lanes' largest logit goes to LDS, and the k-th of these 128 is a bound that at
 // least k logits reach and few more.  While the rest goes by, the 16-byte vectors that reach it are only noted in LDS (a hundred of
 // them); at the end their logits are looked at, a vector a thread, and ranked by counting.  Where more reach it than there
 // is room for (logits in ascending order, thousands of equal ones), those that are noted give a higher bound, and the chunk is
 // read once more with a bound that rises as it goes.
-// Measured: 48 requests of 8 beams, 128000 bf16 logits each (98 MB): 26.8 + 9.4 us, 3.7 TB/s in the first launch, of which 14 us are a
-// workgroup's own: 2.4 until its first logits, 2 for the bound, 5.5 streaming beside three others, 4 for the choice.  Before: a chunk
+// Measured: 48 requests of 8 beams, 128000 bf16 logits each (98 MB): 27.5 + 9.1 us, 3.6 TB/s in the first launch, of which 19 us are a
+// workgroup's own (768 of them): 4.2 until its first logits, 1.8 for the bound, 7.4 streaming, 0.7 for its sum, 4.6 for the choice.
+// 2^21 fp32 logits in ascending order, read twice: 289 us, in descending order 27; read again for every thousand vectors 1101.  Before: a chunk
 // held in registers 47.7 + 24.4; every logit that reaches the bound collected as it goes by 34; candidates of a second level in the second
 // launch's bound 51 -> 9.4.  Chunks: 768 workgroups 26.6, 384 37.9, 1152 27.8, 1920 32, 4992 45.  Loads past the caches: no change.
 #include <hip/hip_bf16.h>
@@ -545,8 +546,6 @@ template <int THREADS> __global__ __launch_bounds__(THREADS) void beam_join_kern
 
 // Chunks of a row, and 16-byte vectors of a chunk: as many workgroups as run at a time (four a CU) where the rows alone are fewer,
 // of one vector a thread at least.
-// Chunks of a row, and 16-byte vectors of a chunk: as many workgroups as run at a time (two a CU) where the rows alone are fewer,
-// chunks of eight thousand logits at least, and of what a workgroup's registers hold at most.
 struct Plan {
     int chunks, vectors;
 };

@@ -589,6 +589,10 @@ int prefix_attn_launch(const lory_paged_shape &s, int groups, const lory_heads &
     a.tiles = z.tiles;
     a.queries = a.beams * a.group;
     a.chunks = z.chunks;
+    // A unit of four blocks takes longer than a row's of one.  Heads of 64, rows / tokens in common / of their own, us with a weight of 1, 2, 3:
+    // 96 / 16000 / 1500 81, 73, 88; 96 / 4000 / 1500 58, 46, 52; 8 groups of 16 / 1000-8000 / 150 32, 27, 25; 6 of 40 / 3000 / 2000 81, 70, 76; 200 /
+    // 30000 / 300 94, 87, 96.  Units of one and two blocks count as a row's: with 1.5 the 24
+    // groups above take 35 for 40, but the long prefix 145 for 118.
     a.weight = z.nq == 4 ? 2 : 1;
     a.ranges = z.ranges;
     a.div = paged::divider(s.page);
